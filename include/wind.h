@@ -354,6 +354,74 @@ typedef struct {
 int wind_get_route_counts(wind_model *m, wind_route_counts *out);
 
 /*
+ * Losses over the output layer, with their gradients: for training a joiner, or a prediction network as a language model, and for
+ * scoring given transcripts.  The output layer is the joiner's W_out / b_out as the caller's program holds it, on the GPU and
+ * changing from step to step (a wind_model is not needed): logits of a row z of H hidden units are x = W z + b, blank is
+ * the last of the V1 outputs.  No call keeps logits or their gradient for all rows: both are formed in pieces inside the workspace.
+ *   dtype       WIND_BF16 or WIND_F32: type of w, of the rows (h, or e and p) and of their gradients; products are summed in fp32,
+ *               fp32 operands are multiplied to 2^-23 relative.  b, db, weights and losses are fp32
+ * Common arguments:
+ *   weights     DEVICE fp32, may be NULL (ones): the gradients are those of the sum over rows (utterances) of weight x loss; the
+ *               losses themselves are not weighted
+ *   dh, de, dp, dw, db   DEVICE, dense, any of them may be NULL (not wanted); they are overwritten
+ *   workspace   DEVICE, 256-byte aligned, at least as many bytes as the query of the same shape says (grads = 1 if a gradient
+ *               is wanted); contents on entry do not matter.  The call enqueues its kernels on `stream` and returns; it allocates
+ *               nothing, does not wait and can be captured.  Calls (and replays of captured ones) that share a workspace must not
+ *               overlap in time
+ * Sums are formed in a fixed order: the same call gives the same bits.  Returns WIND_ERR_ARG for null pointers, sizes out of
+ * range and a missing, misaligned or too small workspace, WIND_ERR_UNSUPPORTED for V1 * H of 2^31 and more, or K above 1024.
+ */
+typedef struct {
+  const void *w;        /* DEVICE [V1, H]                                  */
+  const float *b;       /* DEVICE [V1], or NULL: zeros; -inf bars an output */
+  int64_t w_stride;     /* values between rows of w, at least H            */
+  int32_t V1, H, dtype; /* outputs (labels and blank, >= 2), hidden units  */
+} wind_output_layer;
+
+/* Workspace of wind_label_loss (K = 1) and wind_distill_loss for N rows; HOST pointer.  No GPU work. */
+int wind_row_loss_workspace_bytes(const wind_output_layer *layer, int64_t N, int K, int grads, size_t *bytes);
+
+/*
+ * Cross entropy: loss[n] = log sum_v exp x_v - x_label.  For rows z = h[n]:
+ *   h           DEVICE [N, H], rows h_stride values apart
+ *   labels      DEVICE [N] int32.  A row with a negative label is left out: loss 0, no gradient, its h is not looked at.  One with a
+ *               label >= V1 is left out too, and its loss is NaN
+ *   loss        DEVICE [N] fp32;  dh [N, H], dw [V1, H], db [V1]
+ */
+int wind_label_loss(const wind_output_layer *layer, const void *h, int64_t h_stride, const int32_t *labels, const float *weights, int64_t N, float *loss,
+                    void *dh, void *dw, float *db, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Distillation from a teacher's K largest logits: with q the softmax of a row's teacher logits / temperature over its entries and
+ * p the softmax of x / temperature over all outputs, loss[n] = temperature^2 sum_k q_k (log q_k - log p_label_k).
+ *   teacher_labels, teacher_logits   DEVICE [N, K] int32 / fp32.  Entries with a negative label or a logit of -inf are not there; a row
+ *               without any is left out (loss 0, no gradient); one with a label >= V1 is left out and its loss is NaN.  An output may be named
+ *               twice: both entries count.  (wind_beam_window_scores returns such lists; K <= 1024)
+ */
+int wind_distill_loss(const wind_output_layer *layer, const void *h, int64_t h_stride, const int32_t *teacher_labels, const float *teacher_logits, int K,
+                      float temperature, const float *weights, int64_t N, float *loss, void *dh, void *dw, float *db, void *workspace,
+                      size_t workspace_bytes, void *stream);
+
+int wind_transducer_loss_workspace_bytes(const wind_output_layer *layer, int B, int T, int U, int grads, size_t *bytes);
+
+/*
+ * Transducer loss: loss[b] = -log P(labels[b, 0 .. label_counts[b]) | frames of utterance b), the sum over all ways of placing the labels on
+ * the frames, where a label stays on its frame and blank moves to the next one (rules of Algorithm 1, without its bound on labels
+ * per frame), and the last frame is left by blank.  Node (t, u) has the hidden row z = relu(e[b, t] + p[b, u]).
+ *   e           DEVICE [B, T, H]: encoder halves W_enc f + b_enc; e_stride_b / e_stride_t values between utterances / frames
+ *   p           DEVICE [B, U + 1, H]: prediction halves W_pred g + b_pred after u labels, u = 0 .. U
+ *   labels      DEVICE [B, U] int32, 0 .. V1 - 2
+ *   frames, label_counts   DEVICE [B] int32, clamped to 0 .. T and 0 .. U.  What lies beyond them is not looked at.  An utterance without
+ *               frames is left out (loss 0, no gradient); one with a label that does not exist is left out and its loss is NaN; one of probability zero
+ *               has loss +inf and no gradient
+ *   loss        DEVICE [B] fp32;  de [B, T, H], dp [B, U + 1, H] (zeros beyond frames and label_counts), dw [V1, H], db [V1]
+ * U <= 4095 and B * T * (U + 1) < 2^31 (WIND_ERR_UNSUPPORTED).
+ */
+int wind_transducer_loss(const wind_output_layer *layer, const void *e, int64_t e_stride_b, int64_t e_stride_t, const void *p, int64_t p_stride_b,
+                         int64_t p_stride_u, const int32_t *labels, const int32_t *frames, const int32_t *label_counts, const float *weights, int B, int T,
+                         int U, float *loss, void *de, void *dp, void *dw, float *db, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Tuning knobs, for benchmarks and tests.  key/value pairs:
  *   "graph"   1 (default): the decode loop is replayed from a captured HIP graph; 0: kernels are
  *             launched one by one (the with / without graph rows of Table 5)

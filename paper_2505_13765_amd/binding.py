@@ -18,7 +18,9 @@ EXPORTS = ("wind_load_weights", "wind_free", "wind_greedy_decode", "wind_sequent
            "wind_greedy_decode_async", "wind_get_stats", "wind_debug_joint_logits", "wind_set_option", "wind_last_error",
            "wind_get_kernel_times", "wind_get_joint_launches", "wind_get_call_times", "wind_beam_window_scores", "wind_beam_decode",
            "wind_workspace_bytes", "wind_debug_enc_proj", "wind_debug_joint_keys", "wind_beam_window_scores_static",
-           "wind_get_loop_info", "wind_get_route_counts")
+           "wind_get_loop_info", "wind_get_route_counts",
+           "wind_label_loss", "wind_distill_loss", "wind_row_loss_workspace_bytes", "wind_transducer_loss",
+           "wind_transducer_loss_workspace_bytes")
 PREFIX_MODES = {"off": 0, "keep": 1, "remove": 2}
 KERNEL_NAMES = ("enc_proj", "build_z", "joint", "decide", "lstm", "pred_proj")
 
@@ -63,6 +65,11 @@ class WindRouteCounts(C.Structure):
     ]
 
 
+class OutputLayer(C.Structure):
+    _fields_ = [("w", C.c_void_p), ("b", C.c_void_p), ("w_stride", C.c_int64), ("V1", C.c_int32), ("H", C.c_int32),
+                ("dtype", C.c_int32)]
+
+
 _I32P = C.POINTER(C.c_int32)
 BEAM_ROUND_FN = C.CFUNCTYPE(None, C.c_void_p, C.c_int, C.c_int, C.c_int, _I32P, _I32P, _I32P, C.POINTER(C.c_double), _I32P,
                             C.c_int, _I32P, _I32P, C.POINTER(C.c_float))
@@ -73,6 +80,17 @@ def lib_path() -> str:
 
 
 _lib = None
+
+
+def _declare_losses(lib) -> None:
+    layer, ptr, i64, size = C.POINTER(OutputLayer), C.c_void_p, C.c_int64, C.c_size_t
+    outputs = [ptr, ptr, size, ptr]   # db, workspace and its size, stream
+    lib.wind_row_loss_workspace_bytes.argtypes = [layer, i64, C.c_int, C.c_int, C.POINTER(size)]
+    lib.wind_label_loss.argtypes = [layer, ptr, i64, ptr, ptr, i64, ptr, ptr, ptr, *outputs]
+    lib.wind_distill_loss.argtypes = [layer, ptr, i64, ptr, ptr, C.c_int, C.c_float, ptr, i64, ptr, ptr, ptr, *outputs]
+    lib.wind_transducer_loss_workspace_bytes.argtypes = [layer, C.c_int, C.c_int, C.c_int, C.c_int, C.POINTER(size)]
+    lib.wind_transducer_loss.argtypes = [layer, ptr, i64, i64, ptr, i64, i64, ptr, ptr, ptr, ptr, C.c_int, C.c_int, C.c_int,
+                                         ptr, ptr, ptr, ptr, *outputs]
 
 
 def load_library():
@@ -113,6 +131,7 @@ def load_library():
         lib.wind_beam_decode.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int,
                                          C.c_void_p, C.c_void_p, C.c_int, _I32P, C.POINTER(C.c_double),
                                          C.POINTER(WindBeamStats), C.c_void_p, C.c_void_p, C.c_void_p]
+        _declare_losses(lib)
         _lib = lib
     return _lib
 

@@ -1917,3 +1917,5 @@ int wind_debug_joint_keys(wind_model *m, const float *enc_out, const int32_t *le
 }
 
 }  // extern "C"
+
+#include "wind_loss_api.h"
