@@ -4,35 +4,70 @@
 
 namespace {
 
-using LossBig = LossTile<4, 4, 5>;     // 256 x 256 outputs, one workgroup per CU
-using LossMid = LossTile<2, 2, 4>;     // 128 x 128
-using LossSmall = LossTile<1, 1, 4>;   // 64 x 64
+// Tiles of the products.  rate: of a full chip of them, in parts of kLossRate, for logits and for the products of dx; alone: the part of that left when a CU has one workgroup of them
+// instead of two.  256 x 128 outputs in two workgroups per CU against 256 x 256 in one, sums over 640: 34 us instead of 50 for 5700 rows
+// and 4097 outputs (one's start and results behind the other's products), 1 to 5 % less over 2048; the products of dx, whose sums are
+// longer and whose results cost less: 1.51 ms in one workgroup of 256 x 256, 1.86 in two of 256 x 128 (7373 x 2048 over 65537).
+struct LossShape { int bm, bn; double rate, rate_dx, alone; };
+constexpr LossShape kLossShapes[] = {{256, 256, 0.9, 1.15, 1.0}, {256, 128, 1.0, 1.0, 0.65}, {128, 128, 0.87, 0.87, 0.55}, {64, 64, 0.35, 0.35, 1.0}};
+constexpr LossShape kLossShapesF32[] = {{128, 128, 0.75, 0.75, 1.0}, {64, 64, 0.6, 0.6, 0.65}};
+constexpr double kLossRate = 1.2e15 / 256 / 1e6;   // operations per microsecond and CU
+// the tile of each shape for operands of PA and PB planes
+template <int PA, int PB>
+struct LossTiles;
+template <>
+struct LossTiles<1, 1> {
+  using T0 = LossTile<4, 4, 1, 1, 1, 5, 1>;
+  using T1 = LossTile<4, 2, 1, 1, 1, 3, 2>;
+  using T2 = LossTile<2, 2, 1, 1, 1, 4, 2>;
+  using T3 = LossTile<1, 1, 1, 1, 4, 3, 1>;
+};
+template <>
+struct LossTiles<2, 1> {
+  using T0 = LossTile<4, 4, 2, 1, 1, 3, 1>;
+  using T1 = LossTile<4, 2, 2, 1, 1, 2, 2>;
+  using T2 = LossTile<2, 2, 2, 1, 1, 3, 2>;
+  using T3 = LossTile<1, 1, 2, 1, 2, 3, 1>;
+};
+template <>
+struct LossTiles<3, 3> {
+  using T0 = LossTile<2, 2, 3, 3, 1, 3, 1>;
+  using T1 = LossTile<1, 1, 3, 3, 1, 3, 2>;
+};
 
-constexpr size_t kLossChunkBytes = 512u << 20;   // dx and rows of a chunk, about
+// dx and rows of a chunk, about.  A chunk of 2700 rows of 65537 outputs (512 MB) left the products of few tiles: 8.9 ms for 7373 rows,
+// one chunk 7.4
+constexpr size_t kLossChunkBytes = 1280u << 20;
 constexpr int kLossMaxEntries = 1024;
 
 // the bf16 planes that make up a stored value of each type, and the sum of two bf16 values (hidden rows of the lattice)
 int loss_planes(int dtype) { return dtype == WIND_BF16 ? 1 : 3; }
 int lattice_planes(int dtype) { return dtype == WIND_BF16 ? 2 : 3; }
 
-SegmentsDev loss_segments(int pa, int pb) {
-  SegmentsDev s{0, 0};
-  for (int sum = std::max(pa, pb) - 1; sum >= 0; --sum)
-    for (int i = 0; i < pa; ++i) {
-      const int j = sum - i;
-      if (j < 0 || j >= pb) continue;
-      s.list |= (uint32_t)(i | (j << 2)) << (4 * s.n);
-      ++s.n;
+struct LossPick { int shape, splits, bm, bn; };
+// Shape, and parts of the summed axis, of a product of m x n outputs over `slabs` slabs of 32: the least time of the fullest CU, where a tile costs
+// its operations and about six slabs for its start and its results, and parts cost the writing and reading of their sums.
+LossPick loss_pick(int planes, long long m, long long n, long long slabs, bool split) {
+  const LossShape *shapes = planes == 3 ? kLossShapesF32 : kLossShapes;
+  const int count = planes == 3 ? 2 : 4, products = planes == 3 ? 6 : planes;
+  LossPick best{0, 1, 0, 0};
+  double least = 1e300;
+  for (int t = 0; t < count; ++t) {
+    const LossShape &s = shapes[t];
+    const long long tiles = ((m + s.bm - 1) / s.bm) * ((n + s.bn - 1) / s.bn);
+    for (int parts = 1; parts <= (split ? 64 : 1); ++parts) {
+      if (parts > 1 && (slabs / parts < 8 || tiles * parts > 1024)) break;
+      const long long fullest = (tiles * parts + 255) / 256;
+      const double tile = ((double)((slabs + parts - 1) / parts) * products + 6) * s.bm * s.bn * 64 / (kLossRate * (split ? s.rate_dx : s.rate) * (fullest == 1 ? s.alone : 1.0));
+      const double time = fullest * tile + (parts > 1 ? 1.0 + parts * (double)m * n * 8 / 4e6 : 0.0);
+      if (time < least) {
+        least = time;
+        best = LossPick{t, parts, s.bm, s.bn};
+      }
     }
-  return s;
+  }
+  return best;
 }
-
-// Tile of a product of m x n outputs: the largest whose tiles still reach every CU.
-int loss_tile_size(long long m, long long n) {
-  auto tiles = [&](int t) { return ((m + t - 1) / t) * ((n + t - 1) / t); };
-  return tiles(256) >= 256 ? 256 : tiles(128) >= 256 ? 128 : 64;
-}
-int loss_tile_cols(int tile) { return tile / 2; }   // columns of a wave's block
 
 struct LossPlan {
   int kind, dtype, V1, H, K;
@@ -41,10 +76,11 @@ struct LossPlan {
   int B, T, U;                       // lattice
   // derived
   int R, chunks, vblk, hblk, hd, pa, pw, pd;
-  int tile_x, tile_z, tile_w, splits;
+  LossPick x, z, w;                  // logits, dz, dW
+  bool dw_direct, dz_direct;         // written by their products: one chunk and one part; one part
   // offsets into the workspace
-  size_t idx, count, w, rows, label, value, coef, scale, lse2, logit, part, dx, colsum, dw, total;
-  size_t off, tb, ub, from, nblank, nlabel, nlse2, alpha, beta, dz, de, dp;
+  size_t idx, state, count, wp, rows, label, value, coef, scale, lse2, logit, part, dx, colsum, dw, total;
+  size_t off, tb, ub, arcs, nlse2, alpha, beta, dz, de, dp;
 };
 
 void loss_plan(LossPlan &p) {
@@ -59,11 +95,12 @@ void loss_plan(LossPlan &p) {
   p.chunks = (int)((N + most - 1) / most);
   p.R = (int)round_up((size_t)((N + p.chunks - 1) / p.chunks), 256);
   p.chunks = (int)((N + p.R - 1) / p.R);
-  p.tile_x = loss_tile_size(std::min<long long>(p.R, N), p.V1);
-  p.tile_z = loss_tile_size(std::min<long long>(p.R, N), p.H);
-  p.tile_w = loss_tile_size((long long)p.V1 * 4, p.H);
-  const long long tiles = ((p.V1 + p.tile_w - 1) / p.tile_w) * (long long)((p.H + p.tile_w - 1) / p.tile_w);
-  p.splits = (int)std::max<long long>(1, std::min<long long>((p.tile_w == 256 ? 256 : 512) / tiles, p.R / 256));
+  const long long m = std::min<long long>(p.R, N);
+  p.x = loss_pick(p.pa, m, p.V1, p.hblk, false);
+  p.z = loss_pick(p.pd, m, p.H, p.vblk, true);
+  p.w = loss_pick(p.pd, p.V1, p.H, (m + 31) / 32, true);
+  p.dw_direct = p.chunks == 1 && p.w.splits == 1;
+  p.dz_direct = p.kind != kLossLattice && p.z.splits == 1;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t here = at;
@@ -72,35 +109,38 @@ void loss_plan(LossPlan &p) {
   };
   const size_t R = (size_t)p.R, n = (size_t)N;
   p.count = take(4);
-  p.w = take((size_t)p.pw * p.vblk * 32 * p.hblk * 64);
+  p.wp = take((size_t)p.pw * p.vblk * 32 * p.hblk * 64);
   p.rows = take((size_t)p.pa * R * p.hblk * 64);
   p.label = take(R * p.K * 4);
   p.logit = take(R * p.K * 4);
   p.coef = take(R * p.K * 4);
   p.scale = take(R * 4);
   p.lse2 = take(R * 4);
-  p.part = take(R * 8 * ((p.V1 + loss_tile_cols(p.tile_x) - 1) / loss_tile_cols(p.tile_x)));
-  if (p.kind != kLossLattice) p.idx = take(n * 4);
+  p.part = take(R * 8 * ((p.V1 + p.x.bn / 2 - 1) / (p.x.bn / 2)));
+  if (p.kind != kLossLattice) {
+    p.idx = take(n * 4);
+    p.state = take(n);
+  }
   if (p.kind == kLossDistill) p.value = take(R * p.K * 4);
   if (p.kind == kLossLattice) {
     p.off = take(((size_t)p.B + 1) * 4);
     p.tb = take((size_t)p.B * 4);
     p.ub = take((size_t)p.B * 4);
-    p.from = take(R * 8);
-    p.nblank = take(n * 4);
-    p.nlabel = take(n * 4);
+    p.arcs = take(n * 16);
     p.nlse2 = take(n * 4);
   }
   if (p.grads) {
     p.dx = take((size_t)p.pd * R * p.vblk * 64);
-    p.colsum = take(2 * ((R + p.tile_x - 1) / p.tile_x) * p.vblk * 128);
-    p.dw = take((size_t)p.splits * p.V1 * p.hd * 4);
+    p.colsum = take(2 * ((R + p.x.bm - 1) / p.x.bm) * p.vblk * 128);
+    p.dw = p.dw_direct ? at : take((size_t)p.w.splits * p.V1 * p.hd * 4);
+    p.dz = p.dz_direct ? at : take((size_t)p.z.splits * R * p.hd * 4);
     if (p.kind == kLossLattice) {
       p.alpha = take(n * 8);
       p.beta = take(n * 8);
-      p.dz = take(R * p.hd * 4);
-      p.de = take((size_t)p.B * p.T * p.hd * 4);
-      p.dp = take((size_t)p.B * (p.U + 1) * p.hd * 4);
+      if (p.chunks > 1) {
+        p.de = take((size_t)p.B * p.T * p.hd * 4);
+        p.dp = take((size_t)p.B * (p.U + 1) * p.hd * 4);
+      }
     }
   }
   p.total = at;
@@ -129,13 +169,33 @@ int loss_rows_limits(const LossPlan &p) {
 }
 
 unsigned loss_blocks(size_t items, size_t per = 256, size_t most = 4096) { return (unsigned)std::max<size_t>(1, std::min(most, (items + per - 1) / per)); }
-unsigned loss_grid(long long rt, long long ct) { return (unsigned)((rt * ct + 7) / 8 * 8); }
+unsigned loss_grid(long long rt, long long ct, int splits = 1) { return (unsigned)((rt * ct * splits + 7) / 8 * 8); }
 
 template <class F>
-void loss_with_tile(int tile, F &&f) {
-  if (tile == 256) f(LossBig{});
-  else if (tile == 128) f(LossMid{});
-  else f(LossSmall{});
+void loss_with_tile(int pa, int shape, F &&f) {
+  if (pa == 3) {
+    if (shape == 0) f(LossTiles<3, 3>::T0{});
+    else f(LossTiles<3, 3>::T1{});
+  } else if (pa == 2) {
+    if (shape == 0) f(LossTiles<2, 1>::T0{});
+    else if (shape == 1) f(LossTiles<2, 1>::T1{});
+    else if (shape == 2) f(LossTiles<2, 1>::T2{});
+    else f(LossTiles<2, 1>::T3{});
+  } else {
+    if (shape == 0) f(LossTiles<1, 1>::T0{});
+    else if (shape == 1) f(LossTiles<1, 1>::T1{});
+    else if (shape == 2) f(LossTiles<1, 1>::T2{});
+    else f(LossTiles<1, 1>::T3{});
+  }
+}
+// products of dx: no sums of two values among them
+template <class F>
+void loss_with_dx_tile(int pd, int shape, F &&f) {
+  if (pd == 3) loss_with_tile(3, shape, f);
+  else if (shape == 0) f(LossTiles<1, 1>::T0{});
+  else if (shape == 1) f(LossTiles<1, 1>::T1{});
+  else if (shape == 2) f(LossTiles<1, 1>::T2{});
+  else f(LossTiles<1, 1>::T3{});
 }
 
 struct LossRun {                     // what the launches of one call share
@@ -150,9 +210,10 @@ struct LossRun {                     // what the launches of one call share
   U *at(size_t offset) const { return reinterpret_cast<U *>(ws + offset); }
 };
 
-void loss_begin(LossRun &r) {
+// what the launches of a call share; the packing of W, which its first one does
+LossPack loss_begin(LossRun &r) {
   const LossPlan &p = r.p;
-  r.w = PanelsDev{r.at<bf16_t>(p.w), (size_t)p.vblk * 32 * p.hblk * 32, (uint32_t)p.vblk * 32, (uint32_t)p.hblk};
+  r.w = PanelsDev{r.at<bf16_t>(p.wp), (size_t)p.vblk * 32 * p.hblk * 32, (uint32_t)p.vblk * 32, (uint32_t)p.hblk};
   r.x = PanelsDev{r.at<bf16_t>(p.rows), (size_t)p.R * p.hblk * 32, (uint32_t)p.R, (uint32_t)p.hblk};
   LossChunk &k = r.chunk;
   k.R = p.R;
@@ -173,61 +234,70 @@ void loss_begin(LossRun &r) {
   w.dtype = l.dtype;
   w.rows = l.V1;
   w.cols = l.H;
-  w.dst = r.at<bf16_t>(p.w);
+  w.dst = r.at<bf16_t>(p.wp);
   w.plane = r.w.plane;
   w.dst_rows = p.vblk * 32;
   w.blocks = p.hblk;
   w.planes = p.pw;
   w.vec = (uintptr_t)l.w % 16 == 0 && l.w_stride % 8 == 0;
-  loss_pack_kernel<<<loss_blocks((size_t)w.dst_rows * p.hblk * 4), 256, 0, r.s>>>(w);
+  return w;
 }
 
-LossProduct loss_logits(const LossRun &r) {
-  const LossPlan &p = r.p;
-  return LossProduct{r.x, r.w, loss_segments(p.pa, p.pw), p.hblk, p.V1, (p.V1 + p.tile_x - 1) / p.tile_x, 8};
-}
+LossProduct loss_logits(const LossRun &r) { return LossProduct{r.x, r.w, r.p.hblk, r.p.V1, (r.p.V1 + r.p.x.bn - 1) / r.p.x.bn}; }
 void loss_stats(const LossRun &r, LossNodes nodes) {
   const LossPlan &p = r.p;
   const LossProduct g = loss_logits(r);
-  loss_with_tile(p.tile_x, [&](auto t) {
+  loss_with_tile(p.pa, p.x.shape, [&](auto t) {
     using T = decltype(t);
     loss_stats_kernel<T><<<loss_grid((p.R + T::BM - 1) / T::BM, g.ct), 256, 0, r.s>>>(g, r.chunk, r.layer->b);
   });
-  loss_rows_done_kernel<<<p.R / 64, 256, 0, r.s>>>(r.rows, r.chunk, (p.V1 + loss_tile_cols(p.tile_x) - 1) / loss_tile_cols(p.tile_x), nodes);
+  loss_rows_done_kernel<<<p.R / 16, 256, 0, r.s>>>(r.rows, r.chunk, (p.V1 + p.x.bn / 2 - 1) / (p.x.bn / 2), nodes);
 }
-// dx and what follows from it
-void loss_gradients(const LossRun &r, LossOut *dz, bool dw, float *db, bool add) {
+// dx and its products; what the chunk's last launch has to do then.  dz: the output of one part (label and distillation rows).
+LossFinish loss_gradients(const LossRun &r, int chunk, bool dz, LossOut dz_out, void *dw, float *db) {
   const LossPlan &p = r.p;
   const LossProduct g = loss_logits(r);
   const LossDx d{r.at<bf16_t>(p.dx), (size_t)p.R * p.vblk * 32, p.pd, p.vblk, db ? r.at<float>(p.colsum) : nullptr};
-  loss_with_tile(p.tile_x, [&](auto t) {
+  loss_with_tile(p.pa, p.x.shape, [&](auto t) {
     using T = decltype(t);
     loss_dx_kernel<T><<<loss_grid((p.R + T::BM - 1) / T::BM, g.ct), 256, 0, r.s>>>(g, r.chunk, r.layer->b, d);
   });
-  if (db)
-    loss_db_kernel<<<(p.V1 + 63) / 64, 1024, 0, r.s>>>(d.colsum, p.vblk * 32, p.V1, p.tile_x, r.chunk, add, db);
+  LossFinish f{};
+  if (db) {
+    f.db = LossDb{d.colsum, p.vblk * 32, p.V1, p.x.bm, chunk > 0, db};
+    f.n_db = (p.V1 + 15) / 16;
+  }
   const PanelsDev dx{d.dx, d.plane, (uint32_t)p.R, (uint32_t)p.vblk};
   if (dz) {
-    const LossProduct q{dx, r.w, loss_segments(p.pd, p.pw), p.vblk, p.H, (p.H + p.tile_z - 1) / p.tile_z, 8};
-    loss_with_tile(p.tile_z, [&](auto t) {
+    LossOut o = dz_out;
+    if (!p.dz_direct) {
+      o = LossOut{r.at<float>(p.dz), (size_t)p.hd, 0, p.H, 1, nullptr, 0, p.z.splits, (size_t)p.R * p.hd};
+      if (p.kind != kLossLattice) {
+        f.dz = LossJoin{r.at<float>(p.dz), p.z.splits, o.part, o.ld, 0, p.H, p.dtype, dz_out.vec, dz_out.idx, dz_out.p};
+        f.n_dz = (int)loss_blocks((size_t)p.R * (p.hd / 4), 256, 1024);
+      }
+    }
+    const LossProduct q{dx, r.w, p.vblk, p.H, (p.H + p.z.bn - 1) / p.z.bn};
+    loss_with_dx_tile(p.pd, p.z.shape, [&](auto t) {
       using T = decltype(t);
-      loss_dz_kernel<T><<<loss_grid((p.R + T::BM - 1) / T::BM, q.ct), 256, 0, r.s>>>(q, r.chunk, *dz);
+      loss_dz_kernel<T><<<loss_grid((p.R + T::BM - 1) / T::BM, q.ct, o.splits), 256, 0, r.s>>>(q, r.chunk, o);
     });
   }
   if (dw) {
-    const LossProduct q{dx, r.x, loss_segments(p.pd, p.pw), 0, p.V1, (p.H + p.tile_w - 1) / p.tile_w, 8};
-    const int rt = (p.V1 + p.tile_w - 1) / p.tile_w;
-    const LossOut o{r.at<float>(p.dw), (size_t)p.hd, 0, p.H, 1, nullptr, nullptr, 0, add};
-    loss_with_tile(p.tile_w, [&](auto t) {
+    const LossProduct q{dx, r.x, 0, p.V1, (p.H + p.w.bn - 1) / p.w.bn};
+    const int vec = (uintptr_t)dw % 16 == 0 && p.H % 4 == 0;
+    LossOut o{r.at<float>(p.dw), (size_t)p.hd, 0, p.H, 1, nullptr, chunk > 0, p.w.splits, (size_t)p.V1 * p.hd};
+    if (p.dw_direct) o = LossOut{dw, (size_t)p.H, p.dtype, p.H, vec, nullptr, 0, 1, 0};
+    else if (chunk + 1 == p.chunks) {
+      f.dw = LossJoin{r.at<float>(p.dw), p.w.splits, o.part, o.ld, p.V1, p.H, p.dtype, vec, nullptr, dw};
+      f.n_dw = (int)loss_blocks((size_t)p.V1 * (p.hd / 4), 256, 2048);
+    }
+    loss_with_dx_tile(p.pd, p.w.shape, [&](auto t) {
       using T = decltype(t);
-      loss_dw_kernel<T><<<loss_grid(rt, q.ct) * p.splits, 256, 0, r.s>>>(q, r.chunk, o, rt, p.splits, (size_t)p.V1 * p.hd);
+      loss_dw_kernel<T><<<loss_grid((p.V1 + T::BM - 1) / T::BM, q.ct, o.splits), 256, 0, r.s>>>(q, r.chunk, o);
     });
   }
-}
-void loss_dw_done(const LossRun &r, void *dw) {
-  const LossPlan &p = r.p;
-  loss_dw_done_kernel<<<loss_blocks((size_t)p.V1 * (p.hd / 4)), 256, 0, r.s>>>(r.at<float>(p.dw), p.splits, (size_t)p.V1 * p.hd, (size_t)p.hd, p.V1, p.H,
-                                                                            p.dtype, dw);
+  return f;
 }
 
 int loss_rows_call(const char *name, const wind_output_layer *layer, const void *h, long long h_stride, LossRowsDev rows, long long N, void *dh, void *dw,
@@ -252,10 +322,12 @@ int loss_rows_call(const char *name, const wind_output_layer *layer, const void 
   rows.V1 = layer->V1;
   rows.idx = r.at<int>(p.idx);
   rows.count = r.at<int>(p.count);
+  rows.state = r.at<unsigned char>(p.state);
   r.rows = rows;
-  loss_rows_kernel<<<1, 1024, 0, s>>>(rows);
-  if (dh && N) loss_zero_rows_kernel<<<(unsigned)((N + 3) / 4), 256, 0, s>>>(rows, dh, p.dtype, p.H);
-  loss_begin(r);
+  const LossPack w = loss_begin(r);
+  const unsigned w_blocks = loss_blocks((size_t)w.dst_rows * p.hblk * 4), states = loss_blocks((size_t)N * std::min(p.K, 64), 256, 1024);
+  loss_begin_kernel<<<w_blocks + states, 256, 0, s>>>(w, (int)w_blocks, rows, dh);
+  loss_compact_kernel<<<1, 1024, 0, s>>>(rows);
   LossPack k{};
   k.src = h;
   k.stride = (size_t)h_stride;
@@ -269,17 +341,17 @@ int loss_rows_call(const char *name, const wind_output_layer *layer, const void 
   k.blocks = p.hblk;
   k.planes = p.pa;
   k.vec = (uintptr_t)h % 16 == 0 && h_stride % 8 == 0;
-  LossOut dz{dh, (size_t)p.H, p.dtype, p.H, dh && (uintptr_t)dh % 16 == 0 && p.H % 4 == 0, nullptr, nullptr, 0, 0};
+  LossOut dz{dh, (size_t)p.H, p.dtype, p.H, dh && (uintptr_t)dh % 16 == 0 && p.H % 4 == 0, nullptr, 0, 1, 0};
   for (int c = 0; c < p.chunks; ++c) {
     k.c0 = r.chunk.c0 = c * p.R;
-    loss_pack_kernel<<<loss_blocks((size_t)p.R * p.hblk * 4), 256, 0, s>>>(k);
-    loss_entries_kernel<<<p.R / 256, 256, 0, s>>>(rows, r.chunk);
+    const unsigned packs = loss_blocks((size_t)p.R * p.hblk * 4), entries = loss_blocks((size_t)p.R * std::min(p.K, 64), 256, 1024);
+    loss_chunk_kernel<<<packs + entries, 256, 0, s>>>(k, (int)packs, rows, r.chunk);
     loss_stats(r, LossNodes{});
     if (!p.grads) continue;
     dz.idx = rows.idx + k.c0;
-    loss_gradients(r, dh ? &dz : nullptr, dw != nullptr, db, c > 0);
+    const LossFinish f = loss_gradients(r, c, dh != nullptr, dz, dw, db);
+    if (f.n_db + f.n_dw + f.n_dz) loss_finish_kernel<<<(unsigned)(f.n_db + f.n_dw + f.n_dz), 256, 0, s>>>(f, r.chunk);
   }
-  if (dw) loss_dw_done(r, dw);
   return check_launch(name);
 }
 
@@ -300,7 +372,7 @@ int lattice_plan(LossPlan &p, const wind_output_layer *layer, int B, int T, int 
   if (rc) return rc;
   if (B < 1 || T < 0 || U < 0) return fail(WIND_ERR_ARG, "B >= 1, T >= 0 and U >= 0 required");
   if (U > 4095) return fail(WIND_ERR_UNSUPPORTED, "U must be at most 4095");
-  if ((double)B * T * (U + 1.0) >= 2147483648.0) return fail(WIND_ERR_UNSUPPORTED, "B * T * (U + 1) must be below 2^31");
+  if ((double)B * T * (U + 1.0) >= 2147483648.0 || (double)B * ((double)T + U + 1.0) * ((layer->H + 255) / 256) >= 2147483648.0) return fail(WIND_ERR_UNSUPPORTED, "B * T * (U + 1) and B * (T + U + 1) * H / 256 must be below 2^31");
   p.kind = kLossLattice;
   p.dtype = layer->dtype;
   p.V1 = layer->V1;
@@ -433,41 +505,46 @@ int wind_transducer_loss(const wind_output_layer *layer, const void *e, int64_t 
   l.tb = r.at<int>(p.tb);
   l.ub = r.at<int>(p.ub);
   l.count = r.at<int>(p.count);
-  l.nodes = LossNodes{r.at<float>(p.nblank), r.at<float>(p.nlabel), r.at<float>(p.nlse2)};
+  l.nodes = LossNodes{r.at<float4>(p.arcs), r.at<float>(p.nlse2)};
+  l.vec = (uintptr_t)e % 16 == 0 && (uintptr_t)p_ % 16 == 0 && e_stride_b % 8 == 0 && e_stride_t % 8 == 0 && p_stride_b % 8 == 0 && p_stride_u % 8 == 0;
   if (p.grads) {
     l.alpha = r.at<float2>(p.alpha);
     l.beta = r.at<float2>(p.beta);
   }
-  lattice_rows_kernel<<<1, 1024, 0, s>>>(l);
-  loss_begin(r);
-  int2 *from = r.at<int2>(p.from);
-  const int vec = (uintptr_t)e % 16 == 0 && (uintptr_t)p_ % 16 == 0 && e_stride_b % 8 == 0 && e_stride_t % 8 == 0 && p_stride_b % 8 == 0 && p_stride_u % 8 == 0;
+  const LossPack w = loss_begin(r);
+  lattice_begin_kernel<<<1 + loss_blocks((size_t)w.dst_rows * p.hblk * 4), 256, 0, s>>>(w, l);
+  // a workgroup's 64 rows are shared by as many as it takes to fill the chip
+  const unsigned across = std::min<unsigned>((unsigned)p.hblk, std::max(1u, 1024u / (unsigned)(p.R / 64)));
   auto rows_of_chunk = [&](int c, int grad) {
     r.chunk.c0 = c * p.R;
-    lattice_entries_kernel<<<p.R / 256, 256, 0, s>>>(l, r.chunk, from, grad);
-    lattice_z_kernel<<<loss_blocks((size_t)p.R * p.hblk * 4), 256, 0, s>>>(l, r.chunk, from, r.at<bf16_t>(p.rows), r.x.plane, p.hblk, p.pa, vec);
+    lattice_chunk_kernel<<<dim3((unsigned)(p.R / 64), across), 256, 0, s>>>(l, r.chunk, grad, r.at<bf16_t>(p.rows), r.x.plane, p.hblk, p.pa);
   };
   for (int c = 0; c < p.chunks; ++c) {
     rows_of_chunk(c, 0);
     loss_stats(r, l.nodes);
   }
-  const int both = p.grads, lanes = U + 1;
-  if (lanes <= 1024) lattice_sums_kernel<1, 8><<<B << both, (unsigned)round_up((size_t)lanes, 64), 0, s>>>(l, both);
-  else if (lanes <= 2048) lattice_sums_kernel<2, 4><<<B << both, (unsigned)round_up((size_t)(lanes + 1) / 2, 64), 0, s>>>(l, both);
-  else lattice_sums_kernel<4, 2><<<B << both, (unsigned)round_up((size_t)(lanes + 3) / 4, 64), 0, s>>>(l, both);
+  const int both = p.grads, cells = U + 1;
+  const unsigned runs = (unsigned)B << both;
+  if (cells <= 64) lattice_sums_kernel<1, 8, false><<<runs, 64, 0, s>>>(l, both);
+  else if (cells <= 128) lattice_sums_kernel<2, 8, false><<<runs, 64, 0, s>>>(l, both);
+  else if (cells <= 256) lattice_sums_kernel<4, 4, false><<<runs, 64, 0, s>>>(l, both);
+  else if (cells <= 1024) lattice_sums_kernel<1, 4, true><<<runs, (unsigned)round_up((size_t)cells, 64), 0, s>>>(l, both);
+  else lattice_sums_kernel<4, 1, true><<<runs, (unsigned)round_up((size_t)(cells + 3) / 4, 64), 0, s>>>(l, both);
   if (p.grads) {
-    float *dz = r.at<float>(p.dz), *de32 = r.at<float>(p.de), *dp32 = r.at<float>(p.dp);
-    LossOut o{dz, (size_t)p.hd, 0, p.H, 1, nullptr, r.at<bf16_t>(p.rows), (size_t)p.R, 0};
-    const unsigned across = (unsigned)((p.hd + 255) / 256);
+    const bool whole = p.chunks == 1;
+    LatticeFold fold{r.at<float>(p.dz), p.hd, p.z.splits, (size_t)p.R * p.hd, {nullptr, nullptr}, {T ? de : nullptr, dp}};
+    if (!whole) {
+      fold.sum[0] = r.at<float>(p.de);
+      fold.sum[1] = r.at<float>(p.dp);
+    }
+    const int columns = (p.hd + 255) / 256, n_e = fold.out[0] ? B * T * columns : 0, n_p = fold.out[1] ? B * (U + 1) * columns : 0;
     for (int c = 0; c < p.chunks; ++c) {
       rows_of_chunk(c, 1);
-      loss_gradients(r, de || dp ? &o : nullptr, dw != nullptr, db, c > 0);
-      if (de && T) lattice_fold_kernel<<<dim3((unsigned)B * (unsigned)T, across), 256, 0, s>>>(l, r.chunk, dz, p.hd, 0, de32);
-      if (dp) lattice_fold_kernel<<<dim3((unsigned)B * (unsigned)(U + 1), across), 256, 0, s>>>(l, r.chunk, dz, p.hd, 1, dp32);
+      const LossFinish f = loss_gradients(r, c, n_e + n_p > 0, LossOut{}, dw, db);
+      const int blocks = f.n_db + f.n_dw + n_e + n_p;
+      if (blocks) lattice_finish_kernel<<<(unsigned)blocks, 256, 0, s>>>(f, r.chunk, l, fold, n_e);
     }
-    if (de && T) lattice_fold_done_kernel<<<loss_blocks((size_t)B * T * p.H), 256, 0, s>>>(l, de32, p.hd, 0, de);
-    if (dp) lattice_fold_done_kernel<<<loss_blocks((size_t)B * (U + 1) * p.H), 256, 0, s>>>(l, dp32, p.hd, 1, dp);
-    if (dw) loss_dw_done(r, dw);
+    if (!whole && n_e + n_p) lattice_done_kernel<<<loss_blocks(((size_t)B * (T + U + 1)) * (p.hd / 4)), 256, 0, s>>>(l, fold);
   }
   return check_launch("transducer loss");
 } catch (const std::exception &ex) {

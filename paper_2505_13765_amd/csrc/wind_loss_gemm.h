@@ -10,14 +10,14 @@
 // Either way a wave-wide load of 1 KB is dense memory, and no matrix is ever stored twice or transposed in memory.
 //
 // More than 16 bits.  A value may be kept as a sum of bf16 planes (x = hi + mid + lo, each the rounding of what the ones before leave: 8,
-// 16 or 24 bits).  A product of two such matrices is a sum of products of planes, computed as one product with a longer K: a list of
-// plane pairs ("segments"), the smallest first.  fp32 operands take the six pairs that reach 2^-24 of the product: 2.5 PFLOP/s over six is
-// 2.6 times the rate of the fp32 matrix instructions.
+// 16 or 24 bits).  A product of two such matrices is a sum of products of planes, the smallest first; a stage holds all planes of its K
+// values, so that each is fetched once.  fp32 operands (three planes each) take the six products that reach 2^-24 of the whole: the bf16
+// matrix rate over six is 2.6 times that of the fp32 matrix instructions.  Hidden rows that are sums of two bf16 values take two planes.
 //
 // Schedule of a wave, as in the wide core (wind_mfma_wide.h): a ring of stages filled by direct-to-LDS buffer loads, S stages ahead.  The
-// MFMAs of a stage's first K step run with the fragment reads of the second woven in; then the wave waits for its own loads of the
-// next stage and its own reads, and meets the others at one barrier; the MFMAs of the second step follow with the next stage's first
-// reads and the loads that refill the stage just left.
+// MFMAs of one K step of 16 run with the fragment reads of the next woven in; before a stage's last K step the wave waits for its own loads
+// of the next stage and its own reads, and meets the others at one barrier; the MFMAs of that step come with the next stage's first reads
+// and the loads that refill the stage just left.
 #pragma once
 #include "wind_mfma_wide.h"
 
@@ -32,38 +32,36 @@ struct PanelsDev {
   size_t plane;
   uint32_t rows, blocks;
 };
-// Plane pairs of a product: 4 bits each, a in the lower two, b in the upper two; the first pair lowest.
-struct SegmentsDev {
-  uint32_t list;
-  int n;
-};
 
-// 64 MI x 64 NI outputs on four waves (2 x 2), a ring of S stages of 32 K values.
-template <int MI_, int NI_, int S_>
+// 64 MI x 64 NI outputs on four waves (2 x 2); PA / PB planes of the operands; a ring of S stages of 32 KPS K values.  W workgroups of it
+// share a CU: while one starts or writes its results, the others multiply.
+template <int MI_, int NI_, int PA_, int PB_, int KPS_, int S_, int W_>
 struct LossTile {
-  static constexpr int MI = MI_, NI = NI_, S = S_;
+  static constexpr int MI = MI_, NI = NI_, PA = PA_, PB = PB_, KPS = KPS_, S = S_, W = W_;
   static constexpr int BM = 64 * MI_, BN = 64 * NI_, NT = 256;
-  static constexpr int STA = BM * 64, STB = BN * 64, RING = S_ * (STA + STB);
+  static constexpr int SLAB = (PA_ * BM + PB_ * BN) * 64, STAGE = KPS_ * SLAB, RING = S_ * STAGE;
   static constexpr int PITCH = 32 * NI_ + 4;                 // floats per row of a wave's tile of logits in LDS
   static constexpr int TILE = 4 * 32 * PITCH * 4;            // all four waves', 32 rows each
   static constexpr int SMEM = RING > TILE ? RING : TILE;
-  static constexpr int L = MI_ + NI_;                        // loads per wave and stage
-  static_assert(SMEM <= 160 * 1024 && (S_ - 1) * L < 64 && S_ >= 2 && S_ <= 5, "LDS, vmcnt range");
+  static constexpr int LS = PA_ * MI_ + PB_ * NI_, L = KPS_ * LS;   // loads per wave and slab, and stage
+  static constexpr int PAIRS = PA_ == 3 && PB_ == 3 ? 6 : PA_ * PB_;
+  static_assert(PAIRS == 6 || PB_ == 1, "products of planes");
+  static_assert(W_ * SMEM <= 160 * 1024 && (S_ - 1) * L < 64 && S_ >= 2, "LDS, vmcnt range");
 };
 
-// acc += A[i0 .., :] B[j0 .., :]^T over K stages s0 .. s1 - 1 of every segment.  TA / TB: the operand's K axis is its panels' rows (its tile
+// acc += A[i0 .., :] B[j0 .., :]^T over K slabs (of 32) s0 .. s1 - 1.  TA / TB: the operand's K axis is its panels' rows (its tile
 // rows are columns of the matrix: a multiple of 32 from i0 / j0).  Rows past the end of an operand are read as its last ones: the caller
-// does not use those outputs.  At least one stage (s0 < s1).  The transposed block is accumulated: acc[mi][ni][r] holds A row 32 mi + (lane & 31) and B row
-// 32 ni + 8 (r / 4) + 4 (lane / 32) + r % 4 of the wave's block.  Leaves LDS free for the caller (all waves have passed).
-template <class T, bool TA, bool TB>
-__device__ __forceinline__ void loss_mainloop(const PanelsDev &a, const PanelsDev &b, const SegmentsDev &seg, int i0, int j0, int s0, int s1,
-                                              unsigned char *smem, f32x16 (&acc)[T::MI][T::NI]) {
+// does not use those outputs.  acc is set by `init`, which runs behind the first loads.  At least one slab (s0 < s1).  The transposed block is
+// accumulated: acc[mi][ni][r] holds A row 32 mi + (lane & 31) and B row 32 ni + 8 (r / 4) + 4 (lane / 32) + r % 4 of the wave's block.  Leaves
+// LDS free for the caller (all waves have passed).
+template <class T, bool TA, bool TB, class Init>
+__device__ __forceinline__ void loss_mainloop(const PanelsDev &a, const PanelsDev &b, int i0, int j0, int s0, int s1, unsigned char *smem,
+                                              f32x16 (&acc)[T::MI][T::NI], Init init) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int wm = wave >> 1, wn = wave & 1;
-  const int stages = (s1 - s0) * seg.n;
-  unsigned char *const lds_a = smem, *const lds_b = smem + T::S * T::STA;
+  const int stages = (s1 - s0 + T::KPS - 1) / T::KPS;
 
-  // where a lane's 16 bytes of load group g (1 KB) lie in a stage
+  // where a lane's 16 bytes of load group g (1 KB) lie in a slab
   auto offset = [&](bool trans, const PanelsDev &x, int row0, int g) -> uint32_t {
     if (trans) {
       uint32_t blk = (uint32_t)(row0 >> 5) + (g >> 1);
@@ -82,33 +80,35 @@ __device__ __forceinline__ void loss_mainloop(const PanelsDev &a, const PanelsDe
   for (int i = 0; i < T::NI; ++i) vb[i] = offset(TB, b, j0, 4 * i + wave);
   const uint32_t step_a = TA ? 2048u : a.rows * 64u, step_b = TB ? 2048u : b.rows * 64u;
   const uint32_t bytes_a = a.rows * 64u * a.blocks, bytes_b = b.rows * 64u * b.blocks;
+  i32x4 rs_a[T::PA], rs_b[T::PB];
+#pragma unroll
+  for (int p = 0; p < T::PA; ++p) rs_a[p] = wide_rsrc(a.p + (size_t)p * a.plane, bytes_a);
+#pragma unroll
+  for (int p = 0; p < T::PB; ++p) rs_b[p] = wide_rsrc(b.p + (size_t)p * b.plane, bytes_b);
 
-  // the next stage to fetch
-  int f_seg = 0, f_s = s0;
-  i32x4 rs_a, rs_b;
-  uint32_t so_a, so_b;
-  auto open_segment = [&]() {
-    const uint32_t pair = (seg.list >> (4 * f_seg)) & 15u;
-    rs_a = wide_rsrc(a.p + (size_t)(pair & 3u) * a.plane, bytes_a);
-    rs_b = wide_rsrc(b.p + (size_t)(pair >> 2) * b.plane, bytes_b);
-    so_a = (uint32_t)s0 * step_a;
-    so_b = (uint32_t)s0 * step_b;
-  };
-  open_segment();
-  auto fetch = [&](int q, int slot) {   // load q of a stage
-    if (q < T::MI) wide_load(rs_a, lds_a + slot * T::STA + (4 * q + wave) * 1024, va[q < T::MI ? q : 0], so_a);
-    else wide_load(rs_b, lds_b + slot * T::STB + (4 * (q - T::MI) + wave) * 1024, vb[q >= T::MI ? q - T::MI : 0], so_b);
-  };
-  // Past the last stage the descriptors are empty: such loads touch no memory (zeros arrive in LDS), and the counts that the wave waits
-  // for stay the same in every stage, without a branch in the loop.
-  auto fetched = [&]() {
-    so_a += step_a;
-    so_b += step_b;
-    if (++f_s == s1) {
-      f_s = s0;
-      if (++f_seg < seg.n) open_segment();
-      else rs_a[2] = rs_b[2] = 0;
+  // Load q of the wave's part of a stage whose first slab is f_s.  Past the last slab the descriptor is empty: such a load touches no memory
+  // (zeros arrive in LDS), and the counts that the wave waits for stay the same in every stage, without a branch in the loop.
+  int f_s = s0;
+  uint32_t so_a = (uint32_t)s0 * step_a, so_b = (uint32_t)s0 * step_b;
+  auto fetch = [&](int q, int slot) {
+    const int k = q / T::LS, x = q % T::LS;
+    unsigned char *const at = smem + slot * T::STAGE + k * T::SLAB + wave * 1024;
+    if (x < T::PA * T::MI) {
+      const int p = x / T::MI, i = x % T::MI;
+      i32x4 rs = rs_a[p];
+      rs[2] = f_s + k < s1 ? rs[2] : 0;
+      wide_load(rs, at + p * (T::BM * 64) + i * 4096, va[i], so_a + (uint32_t)k * step_a);
+    } else {
+      const int y = x - T::PA * T::MI, p = y / T::NI, i = y % T::NI;
+      i32x4 rs = rs_b[p];
+      rs[2] = f_s + k < s1 ? rs[2] : 0;
+      wide_load(rs, at + T::PA * (T::BM * 64) + p * (T::BN * 64) + i * 4096, vb[i], so_b + (uint32_t)k * step_b);
     }
+  };
+  auto fetched = [&]() {
+    f_s += T::KPS;
+    so_a += T::KPS * step_a;
+    so_b += T::KPS * step_b;
   };
 #pragma unroll
   for (int s = 0; s < T::S; ++s) {
@@ -116,13 +116,14 @@ __device__ __forceinline__ void loss_mainloop(const PanelsDev &a, const PanelsDe
     for (int q = 0; q < T::L; ++q) fetch(q, s);
     fetched();
   }
+  init();
 
-  bf16x8 af[2][T::MI], bfr[2][T::NI];
+  bf16x8 af[2][T::PA][T::MI], bfr[2][T::PB][T::NI];
   const int frow = lane & 31, half = lane >> 5;
-  const int c0 = (half ^ ((frow >> 2) & 3)) * 16;                                          // K step 1: bit 5 flipped
+  const int c0 = (half ^ ((frow >> 2) & 3)) * 16;                                                  // K step 1: bit 5 flipped
   const int t0 = (8 * half + ((lane & 15) >> 2)) * 64 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;   // K step 1: + 1024
-  auto frag = [&](bool trans, const unsigned char *stage, int blk, int ks) -> bf16x8 {
-    const unsigned char *at = stage + blk * 2048;
+  auto frag = [&](bool trans, const unsigned char *base, int blk, int ks) -> bf16x8 {
+    const unsigned char *at = base + blk * 2048;
     if (trans) {
       union { s16x4 h[2]; bf16x8 v; } u;
       u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + t0 + ks * 1024));
@@ -131,23 +132,30 @@ __device__ __forceinline__ void loss_mainloop(const PanelsDev &a, const PanelsDe
     }
     return *reinterpret_cast<const bf16x8 *>(at + frow * 64 + (c0 ^ (ks * 32)));
   };
-  constexpr int NREAD = T::MI + T::NI, NMFMA = T::MI * T::NI;
-  auto read_frag = [&](int q, int set, int slot, int ks) {   // in the order the MFMAs want them
-    if (q == 0) af[set][0] = frag(TA, lds_a + slot * T::STA, wm * T::MI, ks);
-    else if (q <= T::NI) bfr[set][q - 1] = frag(TB, lds_b + slot * T::STB, wn * T::NI + q - 1, ks);
-    else af[set][q - T::NI] = frag(TA, lds_a + slot * T::STA, wm * T::MI + q - T::NI, ks);
+  constexpr int NREAD = T::LS, NMFMA = T::PAIRS * T::MI * T::NI, STEPS = 2 * T::KPS;
+  // fragment q of K step `step` of the stage in `slot`
+  auto read_frag = [&](int q, int set, int slot, int step) {
+    const unsigned char *at = smem + slot * T::STAGE + (step >> 1) * T::SLAB;
+    if (q < T::PB * T::NI) bfr[set][q / T::NI][q % T::NI] = frag(TB, at + T::PA * (T::BM * 64) + (q / T::NI) * (T::BN * 64), wn * T::NI + q % T::NI, step & 1);
+    else {
+      const int x = q - T::PB * T::NI;
+      af[set][x / T::MI][x % T::MI] = frag(TA, at + (x / T::MI) * (T::BM * 64), wm * T::MI + x % T::MI, step & 1);
+    }
   };
-  // the MFMAs on register set `set`, the reads of K step ks of the stage in `slot` into the other one (if any), `load(x)` behind MFMA x
-  auto kstep = [&](int set, bool reads, int slot, int ks, auto &&load) {
+  // the MFMAs on register set `set`, the reads of K step `step` of the stage in `slot` into the other one (if any), `load(x)` behind MFMA x
+  auto kstep = [&](int set, bool reads, int slot, int step, auto &&load) {
     constexpr int PER = (NREAD + NMFMA - 1) / NMFMA;
 #pragma unroll
     for (int x = 0; x < NMFMA; ++x) {
-      const int mi = x / T::NI, ni = x % T::NI;
-      acc[mi][ni] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bfr[set][ni], af[set][mi], acc[mi][ni], 0, 0, 0);
+      const int pair = x / (T::MI * T::NI), mi = x % (T::MI * T::NI) / T::NI, ni = x % T::NI;
+      // planes of the pair, the smallest product first: (2, 0) (0, 2) (1, 1) (1, 0) (0, 1) (0, 0), or (1, 0) (0, 0)
+      const int pa = T::PAIRS == 6 ? (pair == 0 ? 2 : pair == 2 || pair == 3 ? 1 : 0) : T::PA - 1 - pair;
+      const int pb = T::PAIRS == 6 ? (pair == 1 ? 2 : pair == 2 || pair == 4 ? 1 : 0) : 0;
+      acc[mi][ni] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bfr[set][pb][ni], af[set][pa][mi], acc[mi][ni], 0, 0, 0);
       if (reads) {
 #pragma unroll
         for (int y = 0; y < PER; ++y)
-          if (x * PER + y < NREAD) read_frag(x * PER + y, set ^ 1, slot, ks);
+          if (x * PER + y < NREAD) read_frag(x * PER + y, set ^ 1, slot, step);
       }
       load(x);
       __builtin_amdgcn_sched_barrier(0);
@@ -161,7 +169,8 @@ __device__ __forceinline__ void loss_mainloop(const PanelsDev &a, const PanelsDe
   for (int q = 0; q < NREAD; ++q) read_frag(q, 0, 0, 0);
   int slot = 0;
   for (int j = 1; j < stages; ++j) {
-    kstep(0, true, slot, 1, none);
+#pragma unroll
+    for (int step = 0; step + 1 < STEPS; ++step) kstep(step & 1, true, slot, step + 1, none);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // my reads of this stage are complete
     wait_vmcnt<(T::S - 2) * T::L>();                     // my loads of the next one have landed
     __builtin_amdgcn_s_barrier();
@@ -178,23 +187,24 @@ __device__ __forceinline__ void loss_mainloop(const PanelsDev &a, const PanelsDe
     fetched();
     slot = next;
   }
-  kstep(0, true, slot, 1, none);
+#pragma unroll
+  for (int step = 0; step + 1 < STEPS; ++step) kstep(step & 1, true, slot, step + 1, none);
   kstep(1, false, slot, 0, none);
   wait_vmcnt<0>();
   __syncthreads();
 }
 
-// Tile number of a workgroup: workgroups reach the XCDs in turn, so that number b of XCD b % 8 takes the (b / 8)-th of a consecutive
-// eighth of the tiles, in groups of `group` tile rows column by column: what one XCD works on at a time shares rows and columns in its L2.
-// Returns false for a workgroup without a tile.
-__device__ __forceinline__ bool loss_tile(int bid, int rt, int ct, int group, int &ti, int &tj) {
-  const long long tiles = (long long)rt * ct, per = (tiles + 7) / 8, at = (bid & 7) * per + (bid >> 3);
-  if ((bid >> 3) >= per || at >= tiles) return false;
-  const long long span = (long long)group * ct;
-  const int g = (int)(at / span), in = (int)(at - g * span);
-  const int rows = rt - g * group < group ? rt - g * group : group;
-  ti = g * group + in % rows;
-  tj = in / rows;
+// Tile of a workgroup.  Workgroups reach the XCDs in turn, so that number b of XCD b % 8 takes the (b / 8)-th of a consecutive eighth of
+// the work: part by part of the summed axis (`splits`), in each the tiles in groups of 8 tile rows column by column.  What one XCD works on at
+// a time then shares rows, columns and K in its L2.  Returns false for a workgroup without a tile.
+__device__ __forceinline__ bool loss_place(int bid, int rt, int ct, int splits, int &ti, int &tj, int &split) {
+  const long long tiles = (long long)rt * ct, work = tiles * splits, per = (work + 7) / 8, at = (bid & 7) * per + (bid >> 3);
+  if ((bid >> 3) >= per || at >= work) return false;
+  split = (int)(at / tiles);
+  const long long in = at - split * tiles, span = 8ll * ct;
+  const int g = (int)(in / span), rest = (int)(in - g * span), rows = rt - 8 * g < 8 ? rt - 8 * g : 8;
+  ti = 8 * g + rest % rows;
+  tj = rest / rows;
   return true;
 }
 

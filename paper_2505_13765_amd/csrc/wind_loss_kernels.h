@@ -33,55 +33,93 @@ struct LossRowsDev {           // what the caller gave for every row (label loss
   const float *weights;        // [N] or null
   float inv_tau, tau;
   float *loss;                 // [N]
+  unsigned char *state;        // [N]
   int *idx, *count;            // rows that count, ascending, and their number
 };
 
-// 0: row n counts; 1: it has no label; 2: it names an output that does not exist
-__device__ __forceinline__ int loss_row_state(const LossRowsDev &r, int n) {
-  if (r.kind == kLossLabel) {
-    const int l = r.labels[n];
-    return l < 0 ? 1 : l < r.V1 ? 0 : 2;
-  }
-  bool some = false;
-  for (int k = 0; k < r.K; ++k) {
-    const int l = r.labels[(size_t)n * r.K + k];
-    if (l >= r.V1) return 2;
-    some |= l >= 0 && r.logits[(size_t)n * r.K + k] != -__builtin_inff();
-  }
-  return some ? 0 : 1;
+// Lanes that share a row's K entries: a power of two, at most a wave.
+__device__ __forceinline__ int loss_group(int K) { return K <= 1 ? 1 : K >= 33 ? 64 : 1 << (32 - __builtin_clz((unsigned)(K - 1))); }
+__device__ __forceinline__ float group_max(float v, int group) {
+  for (int d = 1; d < group; d <<= 1) v = fmaxf(v, __shfl_xor(v, d));
+  return v;
+}
+__device__ __forceinline__ float group_sum(float v, int group) {
+  for (int d = 1; d < group; d <<= 1) v += __shfl_xor(v, d);
+  return v;
 }
 
-// One workgroup: the rows that count, in order; the others' losses.
-__global__ __launch_bounds__(1024) void loss_rows_kernel(LossRowsDev r) {
+// Which rows count: state 1, else 0 and the row's loss (0, or NaN if it names an output that does not exist) and gradient (zeros).
+__device__ __forceinline__ void loss_states(const LossRowsDev &r, int block, int nblocks, void *dh, int dtype, int H) {
+  const int lane = threadIdx.x & 63, group = r.kind == kLossLabel ? 1 : loss_group(r.K), rows = 256 / group;
+  const int l = threadIdx.x & (group - 1);
+  const bool wide = (uintptr_t)dh % 16 == 0 && (size_t)H * (dtype ? 2 : 4) % 16 == 0;
+  for (long long n0 = (long long)block * rows; n0 < r.N; n0 += (long long)nblocks * rows) {
+    const long long n = n0 + threadIdx.x / group;
+    bool some = false, wrong = false;
+    if (n < r.N)
+      for (int k = l; k < r.K; k += group) {
+        const int y = r.labels[(size_t)n * r.K + k];
+        wrong |= y >= r.V1;
+        some |= y >= 0 && (r.kind == kLossLabel || r.logits[(size_t)n * r.K + k] != -__builtin_inff());
+      }
+    for (int d = 1; d < group; d <<= 1) {
+      some |= __shfl_xor((int)some, d) != 0;
+      wrong |= __shfl_xor((int)wrong, d) != 0;
+    }
+    const bool counts = some && !wrong;
+    if (n < r.N && l == 0) {
+      r.state[n] = counts ? 1 : 0;
+      if (!counts) r.loss[n] = wrong ? __builtin_nanf("") : 0.f;
+    }
+    if (!dh) continue;
+    unsigned long long out = __ballot(n < r.N && l == 0 && !counts);   // the wave clears its rows one after the other
+    while (out) {
+      const int at = __builtin_ctzll(out);
+      out &= out - 1;
+      const size_t bytes = (size_t)H * (dtype ? 2 : 4);
+      char *row = (char *)dh + (size_t)(n0 + ((threadIdx.x & ~63) + at) / group) * bytes;
+      if (wide)
+        for (size_t c = lane * 16; c < bytes; c += 1024) *reinterpret_cast<u32x4 *>(row + c) = u32x4{0u, 0u, 0u, 0u};
+      else
+        for (size_t c = lane * 2; c < bytes; c += 128) *reinterpret_cast<uint16_t *>(row + c) = 0;
+    }
+  }
+}
+
+// One workgroup: the rows that count, in order.  A thread looks at 16 rows at a time.
+__global__ __launch_bounds__(1024) void loss_compact_kernel(LossRowsDev r) {
   __shared__ int wave_sum_[16], total_;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   if (tid == 0) total_ = 0;
   __syncthreads();
-  for (int base = 0; base < r.N; base += 1024) {
-    const int n = base + tid;
-    const int state = n < r.N ? loss_row_state(r, n) : 1;
-    const unsigned long long mk = __ballot(state == 0);
-    if (lane == 0) wave_sum_[wave] = __popcll(mk);
+  for (long long base = 0; base < r.N; base += 16384) {
+    const long long n = base + tid * 16;
+    u32x4 st = {0u, 0u, 0u, 0u};
+    if (n < r.N) st = *reinterpret_cast<const u32x4 *>(r.state + n);   // (whole sixteens are allocated)
+    uint32_t bits = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) bits |= ((st[i >> 2] >> (8 * (i & 3))) & 1u) << i;
+    if (n + 16 > r.N) bits &= n < r.N ? (1u << (r.N - n)) - 1u : 0u;
+    const int mine = __popc(bits);
+    int sum = mine;
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(sum, d);
+      if (lane >= d) sum += o;
+    }
+    if (lane == 63) wave_sum_[wave] = sum;
     __syncthreads();
     int at = total_;
     for (int w = 0; w < wave; ++w) at += wave_sum_[w];
-    if (state == 0) r.idx[at + __popcll(mk & ((1ull << lane) - 1ull))] = n;
-    else if (n < r.N) r.loss[n] = state == 1 ? 0.f : __builtin_nanf("");
+    int put = at + sum - mine;
+    while (bits) {
+      r.idx[put++] = (int)n + __builtin_ctz(bits);
+      bits &= bits - 1;
+    }
     __syncthreads();
-    if (tid == 1023) total_ = at + wave_sum_[15];
+    if (tid == 1023) total_ = at + sum;
     __syncthreads();
   }
   if (tid == 0) *r.count = total_;
-}
-
-// Rows of the gradient that do not count: zero.
-__global__ __launch_bounds__(256) void loss_zero_rows_kernel(LossRowsDev r, void *dh, int dtype, int H) {
-  const int n = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (n >= r.N || loss_row_state(r, n) == 0) return;
-  for (int h = threadIdx.x & 63; h < H; h += 64) {
-    if (dtype) ((bf16_t *)dh)[(size_t)n * H + h] = 0;
-    else ((float *)dh)[(size_t)n * H + h] = 0.f;
-  }
 }
 
 // ---- panels -------------------------------------------------------------------------------------
@@ -138,12 +176,12 @@ __device__ __forceinline__ void loss_load8(const LossPack &k, size_t row, int c,
 }
 
 // Matrix rows into panels: a thread moves 8 values, four threads a row's 64 bytes of a panel.
-__global__ __launch_bounds__(256) void loss_pack_kernel(LossPack k) {
+__device__ __forceinline__ void loss_pack(const LossPack &k, int block, int nblocks) {
   const int live = k.idx ? min(max(*k.count - k.c0, 0), k.dst_rows) : k.rows;
   const int used = k.idx ? min((live + 255) & ~255, k.dst_rows) : k.dst_rows;   // rows that the products of this chunk read
   const int chunks = k.blocks * 4;
   const size_t total = (size_t)used * chunks;
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (size_t)gridDim.x * 256) {
+  for (size_t i = (size_t)block * 256 + threadIdx.x; i < total; i += (size_t)nblocks * 256) {
     const int q = (int)(i & 3);
     const size_t rest = i >> 2;
     const int row = (int)(rest % used), blk = (int)(rest / used);
@@ -152,6 +190,12 @@ __global__ __launch_bounds__(256) void loss_pack_kernel(LossPack k) {
     if (row < live && c < k.cols) loss_load8(k, k.idx ? (size_t)k.idx[k.c0 + row] : (size_t)row, c, v);
     loss_split8(v, k.planes, k.dst + (size_t)blk * k.dst_rows * 32 + (size_t)row * 32 + q * 8, k.plane);
   }
+}
+
+// The first launch of a call: W into panels, and behind it which rows count.
+__global__ __launch_bounds__(256) void loss_begin_kernel(LossPack w, int pack_blocks, LossRowsDev r, void *dh) {
+  if ((int)blockIdx.x < pack_blocks) loss_pack(w, (int)blockIdx.x, pack_blocks);
+  else loss_states(r, (int)blockIdx.x - pack_blocks, (int)gridDim.x - pack_blocks, dh, w.dtype, w.cols);
 }
 
 // ---- a chunk's rows: entries and statistics -----------------------------------------------------
@@ -170,50 +214,59 @@ struct LossChunk {
 };
 __device__ __forceinline__ int chunk_rows(const LossChunk &k) { return min(max(*k.count - k.c0, 0), k.R); }
 
-// Entries of label and distillation rows.  A thread a row.
-__global__ __launch_bounds__(256) void loss_entries_kernel(LossRowsDev r, LossChunk k) {
+// Entries of label and distillation rows.
+__device__ __forceinline__ void loss_entries(const LossRowsDev &r, const LossChunk &k, int block, int nblocks) {
   const int live = chunk_rows(k), used = min((live + 255) & ~255, k.R);
-  const int i = blockIdx.x * 256 + threadIdx.x;
-  if (i >= used) return;
-  if (i >= live) {
-    for (int e = 0; e < k.K; ++e) k.label[(size_t)e * k.R + i] = -1;
-    k.scale[i] = 0.f;
-    k.lse2[i] = __builtin_inff();
-    return;
+  const int group = r.kind == kLossLabel ? 1 : loss_group(r.K), rows = 256 / group, l = threadIdx.x & (group - 1);
+  for (int i0 = block * rows; i0 < used; i0 += nblocks * rows) {
+    const int i = i0 + (int)threadIdx.x / group;
+    if (i >= live) {
+      for (int e = l; e < k.K; e += group) k.label[(size_t)e * k.R + i] = -1;
+      if (l == 0) {
+        k.scale[i] = 0.f;
+        k.lse2[i] = __builtin_inff();
+      }
+      continue;
+    }
+    const int n = r.idx[k.c0 + i];
+    const float w = r.weights ? r.weights[n] : 1.f;
+    if (r.kind == kLossLabel) {
+      k.label[i] = r.labels[n];
+      k.coef[i] = k.scale[i] = w;
+      continue;
+    }
+    const int *lab = r.labels + (size_t)n * r.K;
+    const float *lg = r.logits + (size_t)n * r.K;
+    float m = -__builtin_inff(), sum = 0.f;
+    for (int e = l; e < r.K; e += group)
+      if (lab[e] >= 0) m = fmaxf(m, lg[e]);
+    m = group_max(m, group);
+    for (int e = l; e < r.K; e += group)
+      if (lab[e] >= 0) sum += exp2f((lg[e] - m) * k.c);
+    const float l2 = log2f(group_sum(sum, group)), wt = w * r.tau;
+    for (int e = l; e < r.K; e += group) {
+      const bool there = lab[e] >= 0 && lg[e] != -__builtin_inff();
+      const float v = there ? (lg[e] - m) * k.c - l2 : -__builtin_inff();
+      k.label[(size_t)e * k.R + i] = there ? lab[e] : -1;
+      k.value[(size_t)e * k.R + i] = v;
+      k.coef[(size_t)e * k.R + i] = wt * exp2f(v);
+    }
+    if (l == 0) k.scale[i] = wt;
   }
-  const int n = r.idx[k.c0 + i];
-  const float w = r.weights ? r.weights[n] : 1.f;
-  if (r.kind == kLossLabel) {
-    k.label[i] = r.labels[n];
-    k.coef[i] = k.scale[i] = w;
-    return;
-  }
-  const int *lab = r.labels + (size_t)n * r.K;
-  const float *lg = r.logits + (size_t)n * r.K;
-  float m = -__builtin_inff();
-  for (int e = 0; e < r.K; ++e)
-    if (lab[e] >= 0) m = fmaxf(m, lg[e]);
-  float sum = 0.f;
-  for (int e = 0; e < r.K; ++e)
-    if (lab[e] >= 0) sum += exp2f((lg[e] - m) * k.c);
-  const float l2 = log2f(sum), wt = w * r.tau;
-  for (int e = 0; e < r.K; ++e) {
-    const bool there = lab[e] >= 0 && lg[e] != -__builtin_inff();
-    const float v = there ? (lg[e] - m) * k.c - l2 : -__builtin_inff();
-    k.label[(size_t)e * k.R + i] = there ? lab[e] : -1;
-    k.value[(size_t)e * k.R + i] = v;
-    k.coef[(size_t)e * k.R + i] = wt * exp2f(v);
-  }
-  k.scale[i] = wt;
+}
+
+// The first launch of a chunk: its rows into panels, and their entries.
+__global__ __launch_bounds__(256) void loss_chunk_kernel(LossPack h, int pack_blocks, LossRowsDev r, LossChunk k) {
+  if ((int)blockIdx.x < pack_blocks) loss_pack(h, (int)blockIdx.x, pack_blocks);
+  else loss_entries(r, k, (int)blockIdx.x - pack_blocks, (int)gridDim.x - pack_blocks);
 }
 
 // ---- logits: statistics, and the gradient's logits ----------------------------------------------
 struct LossProduct {
   PanelsDev a, b;
-  SegmentsDev seg;
-  int stages;                  // K stages of a segment
+  int slabs;                   // of K, 32 each
   int cols;                    // outputs (V1)
-  int ct, group;               // column tiles, tile rows of a group (loss_tile)
+  int ct;                      // column tiles
 };
 
 // A wave's 32 rows x 32 NI columns of logits in LDS, row-major, for entries that name columns.
@@ -233,13 +286,33 @@ __device__ __forceinline__ void loss_tile_out(const f32x16 (&acc)[T::NI], float 
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
   __builtin_amdgcn_wave_barrier();
 }
-// whether one of the wave's rows has an entry among its columns
+// The first two entries of the lane's rows, and which 32-row blocks of the wave have an entry among its columns.
 template <class T>
-__device__ __forceinline__ bool loss_entry_here(const LossChunk &k, int i, int col0) {
-  bool hit = false;
-  for (int e = 0; e < k.K; ++e) hit |= (unsigned)(k.label[(size_t)e * k.R + i] - col0) < (unsigned)(32 * T::NI);
-  return __any(hit);
-}
+struct LossEntries {
+  int label[T::MI][2];
+  unsigned hit;
+  __device__ __forceinline__ void load(const LossChunk &k, int i0, int col0) {
+    bool in[T::MI];
+#pragma unroll
+    for (int mi = 0; mi < T::MI; ++mi) {
+      label[mi][0] = k.label[i0 + 32 * mi];
+      label[mi][1] = k.K > 1 ? k.label[k.R + i0 + 32 * mi] : -1;
+      in[mi] = inside(label[mi][0] - col0) || inside(label[mi][1] - col0);
+    }
+#pragma unroll 4
+    for (int e = 2; e < k.K; ++e)
+#pragma unroll
+      for (int mi = 0; mi < T::MI; ++mi) in[mi] |= inside(k.label[(size_t)e * k.R + i0 + 32 * mi] - col0);
+    hit = 0;
+#pragma unroll
+    for (int mi = 0; mi < T::MI; ++mi) hit |= __any(in[mi]) ? 1u << mi : 0u;
+  }
+  static __device__ __forceinline__ bool inside(int at) { return (unsigned)at < (unsigned)(32 * T::NI); }
+  // entry e of the lane's row of block mi
+  __device__ __forceinline__ int at(const LossChunk &k, int e, int mi, int i0) const {
+    return e == 0 ? label[mi][0] : e == 1 ? label[mi][1] : k.label[(size_t)e * k.R + i0 + 32 * mi];
+  }
+};
 // accumulators that start as the bias; columns past the end as -inf, which exp2 turns into nothing
 template <class T>
 __device__ __forceinline__ void loss_bias(const float *bias, int cols, int col0, f32x16 (&acc)[T::MI][T::NI]) {
@@ -256,20 +329,24 @@ __device__ __forceinline__ void loss_bias(const float *bias, int cols, int col0,
 }
 
 template <class T>
-__global__ __launch_bounds__(256, 1) void loss_stats_kernel(LossProduct g, LossChunk k, const float *bias) {
+__global__ __launch_bounds__(256, T::W) void loss_stats_kernel(LossProduct g, LossChunk k, const float *bias) {
   __shared__ __attribute__((aligned(256))) unsigned char smem[T::SMEM];
   const int live = chunk_rows(k);
-  int ti, tj;
-  if (!loss_tile((int)blockIdx.x, (live + T::BM - 1) / T::BM, g.ct, g.group, ti, tj)) return;
+  int ti, tj, split;
+  if (!loss_place((int)blockIdx.x, (live + T::BM - 1) / T::BM, g.ct, 1, ti, tj, split)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int col0 = tj * T::BN + (wave & 1) * 32 * T::NI;
+  const int i0 = ti * T::BM + (wave >> 1) * 32 * T::MI + (lane & 31);
   f32x16 acc[T::MI][T::NI];
-  loss_bias<T>(bias, g.cols, col0, acc);
-  loss_mainloop<T, false, false>(g.a, g.b, g.seg, ti * T::BM, tj * T::BN, 0, g.stages, smem, acc);
+  LossEntries<T> entries;
+  loss_mainloop<T, false, false>(g.a, g.b, ti * T::BM, tj * T::BN, 0, g.slabs, smem, acc, [&]() {
+    entries.load(k, i0, col0);
+    loss_bias<T>(bias, g.cols, col0, acc);
+  });
   float *tile = reinterpret_cast<float *>(smem) + wave * 32 * T::PITCH;
 #pragma unroll
   for (int mi = 0; mi < T::MI; ++mi) {
-    const int i = ti * T::BM + ((wave >> 1) * T::MI + mi) * 32 + (lane & 31);
+    const int i = i0 + 32 * mi;
     float m = -__builtin_inff();
 #pragma unroll
     for (int ni = 0; ni < T::NI; ++ni)
@@ -284,27 +361,39 @@ __global__ __launch_bounds__(256, 1) void loss_stats_kernel(LossProduct g, LossC
       for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[mi][ni][r], k.c, -ref));
     sum += xor32_f32(sum);
     if (lane < 32 && col0 < g.cols) k.part[(size_t)(col0 / (32 * T::NI)) * k.R + i] = make_float2(mc, sum);
-    if (loss_entry_here<T>(k, i, col0)) {
+    if (entries.hit >> mi & 1u) {
       loss_tile_out<T>(acc[mi], tile);
       for (int e = lane >> 5; e < k.K; e += 2) {   // a row's entries are shared by its two lanes
-        const int at = k.label[(size_t)e * k.R + i] - col0;
-        if ((unsigned)at < (unsigned)(32 * T::NI)) k.logit[(size_t)e * k.R + i] = tile[(lane & 31) * T::PITCH + at];
+        const int at = entries.at(k, e, mi, i0) - col0;
+        if (entries.inside(at)) k.logit[(size_t)e * k.R + i] = tile[(lane & 31) * T::PITCH + at];
       }
       __builtin_amdgcn_wave_barrier();
     }
   }
 }
 
-// Joins a row's column blocks: 64 rows a workgroup, four threads a row.
-struct LossNodes { float *blank, *label, *lse2; };   // per lattice node: log2 probabilities of its arcs, lse2
+// Joins a row's column blocks: 16 rows a workgroup, 16 threads a row.
+// A probability as mantissa and exponent, m 2^e (wind_loss_lattice.h); zero has an exponent below every other's.
+struct Cell { float m; int e; };
+constexpr int kCellZero = -(1 << 28);
+__device__ __forceinline__ Cell cell_of_log2(float l) {   // 2^l, 1 <= m < 2
+  if (l == -__builtin_inff()) return Cell{0.f, kCellZero};
+  const float f = floorf(l);
+  return Cell{__builtin_amdgcn_exp2f(l - f), (int)f};
+}
+struct LossNodes {
+  float4 *arcs;                // per lattice node: the probabilities of blank and of its label (m, e, m, e; e as bits)
+  float *lse2;
+};
 __global__ __launch_bounds__(256) void loss_rows_done_kernel(LossRowsDev r, LossChunk k, int parts, LossNodes nodes) {
-  __shared__ float sm[4][64], ss[4][64];
-  const int live = chunk_rows(k), lane = threadIdx.x & 63, grp = threadIdx.x >> 6;
-  if ((int)blockIdx.x * 64 >= live) return;
-  const int i = blockIdx.x * 64 + lane;
+  __shared__ float sm[16][16], ss[16][16];
+  const int live = chunk_rows(k), lane = threadIdx.x & 15, grp = threadIdx.x >> 4;
+  if ((int)blockIdx.x * 16 >= live) return;
+  const int i = blockIdx.x * 16 + lane;
   float m = -__builtin_inff(), s = 0.f;
   if (i < live) {
-    for (int p = grp; p < parts; p += 4) {
+#pragma unroll 4
+    for (int p = grp; p < parts; p += 16) {
       const float2 v = k.part[(size_t)p * k.R + i];
       const float top = fmaxf(m, v.x), ref = top == -__builtin_inff() ? 0.f : top;
       s = s * __builtin_amdgcn_exp2f(m - ref) + v.y * __builtin_amdgcn_exp2f(v.x - ref);
@@ -315,18 +404,21 @@ __global__ __launch_bounds__(256) void loss_rows_done_kernel(LossRowsDev r, Loss
   ss[grp][lane] = s;
   __syncthreads();
   if (grp || i >= live) return;
-  float top = fmaxf(fmaxf(sm[0][lane], sm[1][lane]), fmaxf(sm[2][lane], sm[3][lane]));
+  float top = sm[0][lane];
+#pragma unroll
+  for (int q = 1; q < 16; ++q) top = fmaxf(top, sm[q][lane]);
   const float ref = top == -__builtin_inff() ? 0.f : top;
   s = 0.f;
 #pragma unroll
-  for (int q = 0; q < 4; ++q) s += ss[q][lane] * __builtin_amdgcn_exp2f(sm[q][lane] - ref);
+  for (int q = 0; q < 16; ++q) s += ss[q][lane] * __builtin_amdgcn_exp2f(sm[q][lane] - ref);
   const float ls = log2f(s), lse2 = top + ls;
   k.lse2[i] = lse2;
   if (r.kind == kLossLattice) {
     const int n = k.c0 + i;
     nodes.lse2[n] = lse2;
-    nodes.blank[n] = -(__builtin_fmaf(-k.logit[i], k.c, top) + ls);
-    nodes.label[n] = k.label[(size_t)k.R + i] < 0 ? -__builtin_inff() : -(__builtin_fmaf(-k.logit[(size_t)k.R + i], k.c, top) + ls);
+    const Cell stay = cell_of_log2(-(__builtin_fmaf(-k.logit[i], k.c, top) + ls));
+    const Cell take = cell_of_log2(k.label[(size_t)k.R + i] < 0 ? -__builtin_inff() : -(__builtin_fmaf(-k.logit[(size_t)k.R + i], k.c, top) + ls));
+    nodes.arcs[n] = make_float4(stay.m, __int_as_float(stay.e), take.m, __int_as_float(take.e));
     return;
   }
   const int n = r.idx[k.c0 + i];
@@ -352,32 +444,36 @@ struct LossDx {
 };
 
 template <class T>
-__global__ __launch_bounds__(256, 1) void loss_dx_kernel(LossProduct g, LossChunk k, const float *bias, LossDx d) {
+__global__ __launch_bounds__(256, T::W) void loss_dx_kernel(LossProduct g, LossChunk k, const float *bias, LossDx d) {
   __shared__ __attribute__((aligned(256))) unsigned char smem[T::SMEM];
   const int live = chunk_rows(k);
-  int ti, tj;
-  if (!loss_tile((int)blockIdx.x, (live + T::BM - 1) / T::BM, g.ct, g.group, ti, tj)) return;
+  int ti, tj, split;
+  if (!loss_place((int)blockIdx.x, (live + T::BM - 1) / T::BM, g.ct, 1, ti, tj, split)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), half = lane >> 5;
   const int col0 = tj * T::BN + (wave & 1) * 32 * T::NI;
+  const int i0 = ti * T::BM + (wave >> 1) * 32 * T::MI + (lane & 31);
   f32x16 acc[T::MI][T::NI];
-  loss_bias<T>(bias, g.cols, col0, acc);
-  loss_mainloop<T, false, false>(g.a, g.b, g.seg, ti * T::BM, tj * T::BN, 0, g.stages, smem, acc);
+  LossEntries<T> entries;
+  loss_mainloop<T, false, false>(g.a, g.b, ti * T::BM, tj * T::BN, 0, g.slabs, smem, acc, [&]() {
+    entries.load(k, i0, col0);
+    loss_bias<T>(bias, g.cols, col0, acc);
+  });
   float *tile = reinterpret_cast<float *>(smem) + wave * 32 * T::PITCH;
 #pragma unroll
   for (int mi = 0; mi < T::MI; ++mi) {
-    const int i = ti * T::BM + ((wave >> 1) * T::MI + mi) * 32 + (lane & 31);
+    const int i = i0 + 32 * mi;
     const float s = k.scale[i], lse2 = k.lse2[i];
 #pragma unroll
     for (int ni = 0; ni < T::NI; ++ni)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[mi][ni][r] = s * __builtin_amdgcn_exp2f(__builtin_fmaf(acc[mi][ni][r], k.c, -lse2));
-    if (loss_entry_here<T>(k, i, col0)) {
+    if (entries.hit >> mi & 1u) {
       loss_tile_out<T>(acc[mi], tile);
       float *row = tile + (lane & 31) * T::PITCH;
       if (lane < 32)   // one lane a row: an output that is named twice is taken off twice, in order
         for (int e = 0; e < k.K; ++e) {
-          const int at = k.label[(size_t)e * k.R + i] - col0;
-          if ((unsigned)at < (unsigned)(32 * T::NI)) row[at] -= k.coef[(size_t)e * k.R + i];
+          const int at = entries.at(k, e, mi, i0) - col0;
+          if (entries.inside(at)) row[at] -= k.coef[(size_t)e * k.R + i];
         }
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
       __builtin_amdgcn_wave_barrier();
@@ -441,23 +537,6 @@ __global__ __launch_bounds__(256, 1) void loss_dx_kernel(LossProduct g, LossChun
   }
 }
 
-// db: the column sums of all row tiles, 64 columns a workgroup, 16 threads a column.
-__global__ __launch_bounds__(1024) void loss_db_kernel(const float *colsum, int width, int cols, int tile_rows, LossChunk k, int add, float *db) {
-  __shared__ float sums[16][64];
-  const int live = chunk_rows(k);
-  const int parts = 2 * ((live + tile_rows - 1) / tile_rows);
-  const int lane = threadIdx.x & 63, grp = threadIdx.x >> 6, v = blockIdx.x * 64 + lane;
-  float s = 0.f;
-  if (v < cols)
-    for (int p = grp; p < parts; p += 16) s += colsum[(size_t)p * width + v];
-  sums[grp][lane] = s;
-  __syncthreads();
-  if (grp || v >= cols) return;
-  s = 0.f;
-  for (int q = 0; q < 16; ++q) s += sums[q][lane];
-  db[v] = add ? db[v] + s : s;
-}
-
 // ---- products of dx -----------------------------------------------------------------------------
 struct LossOut {
   void *p;
@@ -466,18 +545,18 @@ struct LossOut {
   int cols;
   int vec;                     // four values of a row can be stored at once
   const int *idx;              // null, or row i goes to row idx[i]
-  const bf16_t *mask;          // null, or panels (of mask_rows rows): where they are not above zero, the output is zero
-  size_t mask_rows;
   int add;                     // fp32: added to what is there
+  int splits;                  // > 1: fp32, the s-th part of the sum goes to p + s part
+  size_t part;
 };
 template <class T>
-__device__ __forceinline__ void loss_store(const LossOut &o, const f32x16 (&acc)[T::MI][T::NI], int i0, int rows, int j0) {
+__device__ __forceinline__ void loss_store(const LossOut &o, const f32x16 (&acc)[T::MI][T::NI], int i0, int rows, int j0, int split) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), half = lane >> 5;
 #pragma unroll
   for (int mi = 0; mi < T::MI; ++mi) {
     const int i = i0 + ((wave >> 1) * T::MI + mi) * 32 + (lane & 31);
     if (i >= rows) continue;
-    const size_t at = (size_t)(o.idx ? o.idx[i] : i) * o.ld;
+    const size_t at = (size_t)(o.idx ? o.idx[i] : i) * o.ld + (size_t)split * o.part;
 #pragma unroll
     for (int ni = 0; ni < T::NI; ++ni)
 #pragma unroll
@@ -487,14 +566,6 @@ __device__ __forceinline__ void loss_store(const LossOut &o, const f32x16 (&acc)
         f32x4 v;
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = acc[mi][ni][4 * q + e];
-        if (o.mask) {
-          const u32x2 m = *reinterpret_cast<const u32x2 *>(o.mask + (size_t)(j >> 5) * o.mask_rows * 32 + (size_t)i * 32 + (j & 31));
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t bits = (e & 1) ? m[e >> 1] >> 16 : m[e >> 1] & 0xFFFFu;
-            if (bits == 0) v[e] = 0.f;   // z = relu(..): never below zero
-          }
-        }
         if (o.dtype) {
           bf16_t *d = (bf16_t *)o.p + at + j;
           if (o.vec && j + 4 <= o.cols) *reinterpret_cast<u32x2 *>(d) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
@@ -513,56 +584,114 @@ __device__ __forceinline__ void loss_store(const LossOut &o, const f32x16 (&acc)
   }
 }
 
-// dz = dx W: rows of the chunk against columns of W's panels.
 template <class T>
-__global__ __launch_bounds__(256, 1) void loss_dz_kernel(LossProduct g, LossChunk k, LossOut o) {
+__device__ __forceinline__ void loss_clear(f32x16 (&acc)[T::MI][T::NI]) {
+#pragma unroll
+  for (int mi = 0; mi < T::MI; ++mi)
+#pragma unroll
+    for (int ni = 0; ni < T::NI; ++ni) acc[mi][ni] = f32x16{};
+}
+
+// A product whose K axis several workgroups may share: tiles of o.splits parts.
+template <class T, bool TA, bool TB>
+__device__ __forceinline__ void loss_product(int bid, const LossProduct &g, const LossOut &o, int rows, int slabs, unsigned char *smem) {
+  int ti, tj, split;
+  if (!loss_place(bid, (rows + T::BM - 1) / T::BM, g.ct, o.splits, ti, tj, split)) return;
+  const int per = (slabs + o.splits - 1) / o.splits, s0 = min(split * per, slabs), s1 = min(s0 + per, slabs);
+  f32x16 acc[T::MI][T::NI];
+  if (s0 < s1) loss_mainloop<T, TA, TB>(g.a, g.b, ti * T::BM, tj * T::BN, s0, s1, smem, acc, [&]() { loss_clear<T>(acc); });
+  else loss_clear<T>(acc);
+  loss_store<T>(o, acc, ti * T::BM, rows, tj * T::BN, split);
+}
+// dz = dx W: rows of the chunk against columns of W's panels, summed over outputs.
+template <class T>
+__global__ __launch_bounds__(256, T::W) void loss_dz_kernel(LossProduct g, LossChunk k, LossOut o) {
+  __shared__ __attribute__((aligned(256))) unsigned char smem[T::SMEM];
+  loss_product<T, false, true>((int)blockIdx.x, g, o, chunk_rows(k), g.slabs, smem);
+}
+// dW = dx^T z: columns of dx's panels against columns of z's, summed over the chunk's rows.
+template <class T>
+__global__ __launch_bounds__(256, T::W) void loss_dw_kernel(LossProduct g, LossChunk k, LossOut o) {
   __shared__ __attribute__((aligned(256))) unsigned char smem[T::SMEM];
   const int live = chunk_rows(k);
-  int ti, tj;
-  if (!loss_tile((int)blockIdx.x, (live + T::BM - 1) / T::BM, g.ct, g.group, ti, tj)) return;
-  f32x16 acc[T::MI][T::NI];
-#pragma unroll
-  for (int mi = 0; mi < T::MI; ++mi)
-#pragma unroll
-    for (int ni = 0; ni < T::NI; ++ni) acc[mi][ni] = f32x16{};
-  loss_mainloop<T, false, true>(g.a, g.b, g.seg, ti * T::BM, tj * T::BN, 0, g.stages, smem, acc);
-  loss_store<T>(o, acc, ti * T::BM, live, tj * T::BN);
-}
-
-// dW = dx^T z: columns of dx's panels against columns of z's, summed over the chunk's rows, which `splits` workgroups share.
-template <class T>
-__global__ __launch_bounds__(256, 1) void loss_dw_kernel(LossProduct g, LossChunk k, LossOut o, int rt, int splits, size_t part) {
-  __shared__ __attribute__((aligned(256))) unsigned char smem[T::SMEM];
-  const int live = chunk_rows(k), stages = (live + 31) / 32;
   if (o.add && live == 0) return;
-  const int split = (int)blockIdx.x % splits;
-  int ti, tj;
-  if (!loss_tile((int)blockIdx.x / splits, rt, g.ct, g.group, ti, tj)) return;
-  const int per = (stages + splits - 1) / splits, s0 = min(split * per, stages), s1 = min(s0 + per, stages);
-  f32x16 acc[T::MI][T::NI];
-#pragma unroll
-  for (int mi = 0; mi < T::MI; ++mi)
-#pragma unroll
-    for (int ni = 0; ni < T::NI; ++ni) acc[mi][ni] = f32x16{};
-  if (s0 < s1) loss_mainloop<T, true, true>(g.a, g.b, g.seg, ti * T::BM, tj * T::BN, s0, s1, smem, acc);
-  o.p = (float *)o.p + (size_t)split * part;
-  loss_store<T>(o, acc, ti * T::BM, g.cols, tj * T::BN);
+  loss_product<T, true, true>((int)blockIdx.x, g, o, g.cols, (live + 31) / 32, smem);
 }
 
-// The splits' sums, rounded once.
-__global__ __launch_bounds__(256) void loss_dw_done_kernel(const float *parts, int splits, size_t part, size_t ld, int rows, int cols, int dtype, void *dw) {
-  const int per_row = (cols + 3) / 4;
+// ---- the last launch of a chunk -----------------------------------------------------------------
+// db: the column sums of all row tiles.  A workgroup takes 16 columns, 16 threads each.
+struct LossDb {
+  const float *colsum;
+  int width, cols, tile_rows, add;
+  float *db;
+};
+__device__ __forceinline__ void loss_db(const LossDb &d, int live, int block) {
+  __shared__ float sums[16][16];
+  const int parts = 2 * ((live + d.tile_rows - 1) / d.tile_rows);
+  const int lane = threadIdx.x & 15, grp = threadIdx.x >> 4, v = block * 16 + lane;
+  float s = 0.f;
+  if (v < d.cols) {
+#pragma unroll 8
+    for (int p = grp; p < parts; p += 16) s += d.colsum[(size_t)p * d.width + v];
+  }
+  sums[grp][lane] = s;
+  __syncthreads();
+  if (grp || v >= d.cols) return;
+  s = 0.f;
+#pragma unroll
+  for (int q = 0; q < 16; ++q) s += sums[q][lane];
+  d.db[v] = d.add ? d.db[v] + s : s;
+}
+
+// Sums of a product's parts, rounded once (rows: as many as count where idx is given).
+struct LossJoin {
+  const float *parts;
+  int splits;
+  size_t part, ld;
+  int rows, cols, dtype, vec;
+  const int *idx;
+  void *out;                   // [.., cols]
+};
+__device__ __forceinline__ void loss_join(const LossJoin &j, int rows, int block, int nblocks) {
+  const int per_row = (j.cols + 3) / 4;
   const size_t total = (size_t)rows * per_row;
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (size_t)gridDim.x * 256) {
+  for (size_t i = (size_t)block * 256 + threadIdx.x; i < total; i += (size_t)nblocks * 256) {
     const size_t v = i / per_row;
     const int h = (int)(i - v * per_row) * 4;
-    f32x4 s = *reinterpret_cast<const f32x4 *>(parts + v * ld + h);
-    for (int q = 1; q < splits; ++q) s += *reinterpret_cast<const f32x4 *>(parts + (size_t)q * part + v * ld + h);
-    for (int e = 0; e < 4 && h + e < cols; ++e) {
-      if (dtype) ((bf16_t *)dw)[v * cols + h + e] = (bf16_t)f32_to_bf16_bits(s[e]);
-      else ((float *)dw)[v * cols + h + e] = s[e];
+    f32x4 s = *reinterpret_cast<const f32x4 *>(j.parts + v * j.ld + h);
+    for (int q = 1; q < j.splits; ++q) s += *reinterpret_cast<const f32x4 *>(j.parts + (size_t)q * j.part + v * j.ld + h);
+    const size_t to = (j.idx ? (size_t)j.idx[v] : v) * j.cols + h;
+    if (j.vec) {
+      if (j.dtype) *reinterpret_cast<u32x2 *>((bf16_t *)j.out + to) = u32x2{pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3])};
+      else *reinterpret_cast<f32x4 *>((float *)j.out + to) = s;
+      continue;
+    }
+    for (int e = 0; e < 4 && h + e < j.cols; ++e) {
+      if (j.dtype) ((bf16_t *)j.out)[to + e] = (bf16_t)f32_to_bf16_bits(s[e]);
+      else ((float *)j.out)[to + e] = s[e];
     }
   }
+}
+
+// What is left of a chunk of label or distillation rows: db, and the sums over parts of dW (with the last chunk) and dz.
+struct LossFinish {
+  LossDb db;
+  LossJoin dw, dz;
+  int n_db, n_dw, n_dz;        // workgroups of each
+};
+// false: the workgroup's number, less those taken, is left in `block`
+__device__ __forceinline__ bool loss_finish(const LossFinish &f, const LossChunk &k, int &block) {
+  if (block < f.n_db) { loss_db(f.db, chunk_rows(k), block); return true; }
+  block -= f.n_db;
+  if (block < f.n_dw) { loss_join(f.dw, f.dw.rows, block, f.n_dw); return true; }
+  block -= f.n_dw;
+  if (block < f.n_dz) { loss_join(f.dz, chunk_rows(k), block, f.n_dz); return true; }
+  block -= f.n_dz;
+  return false;
+}
+__global__ __launch_bounds__(256) void loss_finish_kernel(LossFinish f, LossChunk k) {
+  int block = (int)blockIdx.x;
+  loss_finish(f, k, block);
 }
 
 }  // namespace wind

@@ -18,6 +18,7 @@ struct LatticeDev {
   int B, T, U, V1, H, dtype;
   const void *e, *p;                          // e [B, T, H], p [B, U + 1, H]
   long long e_b, e_t, p_b, p_u;               // strides in values
+  int vec;                                    // their rows are 16-byte aligned
   const int *labels, *frames, *counts;        // [B, U], [B], [B]
   const float *weights;                       // [B] or null
   float *loss;                                // [B]
@@ -25,11 +26,14 @@ struct LatticeDev {
   LossNodes nodes;
   float2 *alpha, *beta;                       // per node: mantissa, exponent (int bits)
 };
+__device__ __forceinline__ const char *lattice_e(const LatticeDev &l, int b, int t) { return (const char *)l.e + (b * l.e_b + t * l.e_t) * (l.dtype ? 2 : 4); }
+__device__ __forceinline__ const char *lattice_p(const LatticeDev &l, int b, int u) { return (const char *)l.p + (b * l.p_b + u * l.p_u) * (l.dtype ? 2 : 4); }
 
-__global__ __launch_bounds__(1024) void lattice_rows_kernel(LatticeDev l) {
-  __shared__ int wave_sum_[16], total_;
+// One workgroup: which utterances count, and where their rows begin.
+__device__ __forceinline__ void lattice_rows(const LatticeDev &l) {
+  __shared__ int wave_sum_[4], total_;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  for (int b = wave; b < l.B; b += 16) {
+  for (int b = wave; b < l.B; b += 4) {
     const int T = min(max(l.frames[b], 0), l.T), U = min(max(l.counts[b], 0), l.U);
     bool bad = false;
     for (int u = lane; u < U; u += 64) {
@@ -45,7 +49,7 @@ __global__ __launch_bounds__(1024) void lattice_rows_kernel(LatticeDev l) {
   }
   if (tid == 0) total_ = 0;
   __syncthreads();
-  for (int base = 0; base < l.B; base += 1024) {
+  for (int base = 0; base < l.B; base += 256) {
     const int b = base + tid;
     const int n = b < l.B ? l.tb[b] * (l.ub[b] + 1) : 0;
     int sum = n;
@@ -59,7 +63,7 @@ __global__ __launch_bounds__(1024) void lattice_rows_kernel(LatticeDev l) {
     for (int w = 0; w < wave; ++w) at += wave_sum_[w];
     if (b < l.B) l.off[b] = at + sum - n;
     __syncthreads();
-    if (tid == 1023) total_ = at + sum;
+    if (tid == 255) total_ = at + sum;
     __syncthreads();
   }
   if (tid == 0) {
@@ -67,85 +71,88 @@ __global__ __launch_bounds__(1024) void lattice_rows_kernel(LatticeDev l) {
     *l.count = total_;
   }
 }
+// The first launch of a call: the rows, and W into panels.
+__global__ __launch_bounds__(256) void lattice_begin_kernel(LossPack w, LatticeDev l) {
+  if (blockIdx.x == 0) lattice_rows(l);
+  else loss_pack(w, (int)blockIdx.x - 1, (int)gridDim.x - 1);
+}
 
-struct Cell { float m; int e; };
-constexpr int kCellZero = -(1 << 28);
-__device__ __forceinline__ Cell cell_of_log2(float l) {   // 2^l
-  const float f = floorf(l);
-  if (l == -__builtin_inff()) return Cell{0.f, kCellZero};
-  return Cell{__builtin_amdgcn_exp2f(l - f), (int)f};
+// a + b.  An exponent never falls below that of zero, so that sums of exponents stay in range.
+__device__ __forceinline__ Cell cell_sum(Cell a, Cell b) {
+  const int e = max(max(a.e, b.e), kCellZero);
+  const float m = __builtin_amdgcn_ldexpf(a.m, a.e - e) + __builtin_amdgcn_ldexpf(b.m, b.e - e);
+  return Cell{__builtin_amdgcn_frexp_mantf(m), e + __builtin_amdgcn_frexp_expf(m)};
 }
-__device__ __forceinline__ Cell cell_step(Cell a, Cell pa, Cell b, Cell pb) {   // a pa + b pb
-  const float m1 = a.m * pa.m, m2 = b.m * pb.m;
-  const int e1 = a.e + pa.e, e2 = b.e + pb.e, e = max(e1, e2);
-  const float m = ldexpf(m1, e1 - e) + ldexpf(m2, e2 - e);
-  return Cell{__builtin_amdgcn_frexp_mantf(m), m == 0.f ? kCellZero : e + __builtin_amdgcn_frexp_expf(m)};
-}
+__device__ __forceinline__ Cell cell_product(Cell a, Cell b) { return Cell{a.m * b.m, a.e + b.e}; }
 __device__ __forceinline__ float2 cell_pack(Cell c) { return make_float2(c.m, __int_as_float(c.e)); }
 __device__ __forceinline__ Cell cell_unpack(float2 v) { return Cell{v.x, __float_as_int(v.y)}; }
 
 // One workgroup runs one utterance's recursion, alpha or beta (mirrored: t' = T - 1 - t, u' = U - u), along diagonals: thread i owns C
-// consecutive u, is one frame behind thread i - 1, and takes its neighbour's last cell from LDS.  The nodes' probabilities of the
-// next AHEAD frames are requested before the present ones are worked off.
-template <int C, int AHEAD>
-__global__ __launch_bounds__(1024) void lattice_sums_kernel(LatticeDev l, int both) {
-  __shared__ float2 edge[2][1025];
+// consecutive u, is one frame behind thread i - 1, and takes what its neighbour's last cell hands on from the lane before it, or, in a
+// workgroup of several waves (MULTI), from LDS at a wave's edge.  Cells outside the lattice need no branch: before its first frame a
+// thread's inputs are zero, and what is computed past the last frame or label reaches no cell that counts.  The next AHEAD
+// frames' arcs are on their way while the present ones are worked off.
+// The time is the number of diagonals, T + U / C, times C dependent steps of about 40 cycles and their issue: 750 frames and 120 labels
+// (C = 2) ran 529 us with logarithms converted on the way, a barrier and LDS per diagonal.
+template <int C, int AHEAD, bool MULTI>
+__global__ __launch_bounds__(MULTI ? 1024 : 64) void lattice_sums_kernel(LatticeDev l, int both) {
+  __shared__ float2 edge[2][17];
   const int b = both ? (int)blockIdx.x >> 1 : (int)blockIdx.x;
   const bool fwd = both && (blockIdx.x & 1);
-  const int T = l.tb[b], U1 = l.ub[b] + 1, off = l.off[b], tid = threadIdx.x;
+  const int T = l.tb[b], U1 = l.ub[b] + 1, off = l.off[b], tid = threadIdx.x, wave = tid >> 6;
   if (T == 0) return;
   const int lanes = (U1 + C - 1) / C, steps = T + lanes - 1;
-  // arcs that lead into cell (t', u') of this direction
-  auto arcs = [&](int t, int j, float &up, float &left) {
-    const int u = tid * C + j;
-    up = left = -__builtin_inff();
-    if (t < 0 || t >= T || u >= U1) return;
-    if (fwd) {
-      if (t > 0) up = l.nodes.blank[off + (t - 1) * U1 + u];
-      else if (u == 0) up = 0.f;
-      if (u > 0) left = l.nodes.label[off + t * U1 + u - 1];
-    } else {
-      const int n = off + (T - 1 - t) * U1 + (U1 - 1 - u);
-      if (t > 0 || u == 0) up = l.nodes.blank[n];
-      if (u > 0) left = l.nodes.label[n];
-    }
+  // this thread's nodes: cell (t', u' = tid C + j)
+  auto node = [&](int t, int j) {
+    const int u = min(tid * C + j, U1 - 1), tc = min(max(t, 0), T - 1);
+    return off + (fwd ? tc * U1 + u : (T - 1 - tc) * U1 + (U1 - 1 - u));
   };
-  Cell row[C];   // cells (t - 1, .) of this thread
+  Cell up[C], out{0.f, kCellZero};       // what comes from the frame before; what the last cell hands on
 #pragma unroll
-  for (int j = 0; j < C; ++j) row[j] = (tid == 0 && j == 0) ? Cell{0.5f, 1} : Cell{0.f, kCellZero};
-  float up[2][AHEAD][C], left[2][AHEAD][C];
+  for (int j = 0; j < C; ++j) up[j] = (tid == 0 && j == 0) ? Cell{0.5f, 1} : Cell{0.f, kCellZero};
+  float4 arcs[2][AHEAD][C];
   auto request = [&](int set, int d0) {
 #pragma unroll
     for (int s = 0; s < AHEAD; ++s)
 #pragma unroll
-      for (int j = 0; j < C; ++j) arcs(d0 + s - tid, j, up[set][s][j], left[set][s][j]);
+      for (int j = 0; j < C; ++j) arcs[set][s][j] = l.nodes.arcs[node(d0 + s - tid, j)];
   };
   auto work = [&](int set, int d0) {
 #pragma unroll
     for (int s = 0; s < AHEAD; ++s) {
       const int d = d0 + s, t = d - tid;
-      const bool here = t >= 0 && t < T;
-      Cell before = (tid > 0) ? cell_unpack(edge[d & 1][tid]) : Cell{0.f, kCellZero};
+      // the neighbour's, one diagonal ago
+      Cell left;
+      left.m = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, out.m), 0x138, 0xF, 0xF, false));
+      left.e = __builtin_amdgcn_update_dpp(kCellZero, out.e, 0x138, 0xF, 0xF, false);
+      if (MULTI) {
+        if ((tid & 63) == 63) edge[d & 1][wave + 1] = cell_pack(out);
+        __syncthreads();
+        if ((tid & 63) == 0) left = cell_unpack(edge[d & 1][wave]);
+      }
 #pragma unroll
       for (int j = 0; j < C; ++j) {
-        const int u = tid * C + j;
-        const Cell v = cell_step(row[j], cell_of_log2(up[set][s][j]), before, cell_of_log2(left[set][s][j]));
-        if (here && u < U1) {
-          row[j] = v;
-          if (fwd) l.alpha[off + t * U1 + u] = cell_pack(v);
-          else if (both) l.beta[off + (T - 1 - t) * U1 + (U1 - 1 - u)] = cell_pack(v);
-          if (!fwd && t == T - 1 && u == U1 - 1)
-            l.loss[b] = (float)(-(log2((double)v.m) + (double)v.e) * kLn2);
-          before = v;
+        const float4 a = arcs[set][s][j];
+        const Cell stay{a.x, __float_as_int(a.y)}, take{a.z, __float_as_int(a.w)};
+        Cell v;
+        if (fwd) {                        // hands on what its own arcs make of it
+          v = cell_sum(up[j], left);
+          up[j] = cell_product(v, stay);
+          left = cell_product(v, take);
+        } else {                          // its own arcs make it of what it is handed
+          v = cell_sum(cell_product(up[j], stay), cell_product(left, take));
+          up[j] = left = v;
         }
+        const bool here = t >= 0 && t < T && tid * C + j < U1;
+        if (here && both) (fwd ? l.alpha : l.beta)[node(t, j)] = cell_pack(v);
+        if (here && !fwd && t == T - 1 && tid * C + j == U1 - 1) l.loss[b] = (float)(-(log2((double)v.m) + (double)v.e) * kLn2);
       }
-      edge[(d + 1) & 1][tid + 1] = cell_pack(before);
-      __syncthreads();
+      out = left;
     }
   };
-  edge[0][tid] = edge[1][tid] = make_float2(0.f, __int_as_float(kCellZero));
+  if (MULTI && tid < 34) edge[tid & 1][tid >> 1] = make_float2(0.f, __int_as_float(kCellZero));
   request(0, 0);
-  __syncthreads();
+  if (MULTI) __syncthreads();
   for (int d0 = 0; d0 < steps; d0 += 2 * AHEAD) {
     request(1, d0 + AHEAD);
     work(0, d0);
@@ -154,111 +161,160 @@ __global__ __launch_bounds__(1024) void lattice_sums_kernel(LatticeDev l, int bo
   }
 }
 
-// A chunk's rows: where they take e and p from, their two entries (0: blank, 1: the next label), and for the gradient the arcs' expected counts.
-__global__ __launch_bounds__(256) void lattice_entries_kernel(LatticeDev l, LossChunk k, int2 *from, int grad) {
+// The first launch of a chunk: its rows z = relu(e + p) in panels, their two entries (0: blank, 1: the next label), and for the gradient
+// the arcs' expected counts.  A workgroup takes 64 rows, four threads a row.
+__global__ __launch_bounds__(256) void lattice_chunk_kernel(LatticeDev l, LossChunk k, int grad, bf16_t *dst, size_t plane, int blocks, int planes) {
   const int live = chunk_rows(k), used = min((live + 255) & ~255, k.R);
-  const int i = blockIdx.x * 256 + threadIdx.x;
+  const int i = blockIdx.x * 64 + (threadIdx.x >> 2), q = threadIdx.x & 3;
   if (i >= used) return;
+  bf16_t *to = dst + (size_t)i * 32 + q * 8;
   if (i >= live) {
-    from[i] = make_int2(-1, -1);
-    k.label[i] = k.label[k.R + i] = -1;
-    k.scale[i] = 0.f;
-    k.lse2[i] = __builtin_inff();
+    const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int blk = blockIdx.y; blk < blocks; blk += gridDim.y) loss_split8(none, planes, to + (size_t)blk * k.R * 32, plane);
+    if (q == 0 && blockIdx.y == 0) {
+      k.label[i] = k.label[k.R + i] = -1;
+      k.scale[i] = 0.f;
+      k.lse2[i] = __builtin_inff();
+    }
     return;
   }
   const int n = k.c0 + i;
-  int lo = 0, hi = l.B;          // the last utterance whose first row is at or before n and that has rows
+  int lo = 0, hi = l.B;          // the last utterance whose first row is at or before n: it has rows
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     if (l.off[mid] <= n) lo = mid;
     else hi = mid;
   }
   const int b = lo, U1 = l.ub[b] + 1, at = n - l.off[b], t = at / U1, u = at - t * U1;
-  from[i] = make_int2(b * l.T + t, b * (l.U + 1) + u);
+  LossPack e{}, p{};
+  e.dtype = p.dtype = l.dtype;
+  e.cols = p.cols = l.H;
+  e.vec = p.vec = l.vec;
+  e.src = lattice_e(l, b, t);
+  p.src = lattice_p(l, b, u);
+  for (int blk = blockIdx.y; blk < blocks; blk += gridDim.y) {
+    const int c = blk * 32 + q * 8;
+    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (c < l.H) {
+      float y[8];
+      loss_load8(e, 0, c, x);
+      loss_load8(p, 0, c, y);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) { x[j] += y[j]; x[j] = x[j] > 0.f || x[j] != x[j] ? x[j] : 0.f; }   // NaN stays
+    }
+    loss_split8(x, planes, to + (size_t)blk * k.R * 32, plane);
+  }
+  if (q || blockIdx.y) return;
   k.label[i] = l.V1 - 1;
   k.label[k.R + i] = u + 1 < U1 ? l.labels[(size_t)b * l.U + u] : -1;
   if (!grad) return;
   const Cell P = cell_unpack(l.beta[l.off[b]]), a = cell_unpack(l.alpha[n]);
+  const float4 arcs = l.nodes.arcs[n];
   const float w = l.weights ? l.weights[b] : 1.f;
-  auto share = [&](float arc, Cell to) {   // expected count of an arc, times the utterance's weight
-    const Cell q = cell_of_log2(arc);
-    return P.m == 0.f ? 0.f : w * ldexpf(a.m * q.m * to.m / P.m, a.e + q.e + to.e - P.e);
+  auto share = [&](float m, float e_bits, Cell next) {   // expected count of an arc, times the utterance's weight
+    return P.m == 0.f ? 0.f : w * __builtin_amdgcn_ldexpf(a.m * m * next.m / P.m, a.e + __float_as_int(e_bits) + next.e - P.e);
   };
-  const bool last = t + 1 == l.tb[b];
-  const float by_blank = last ? (u + 1 == U1 ? share(l.nodes.blank[n], Cell{0.5f, 1}) : 0.f) : share(l.nodes.blank[n], cell_unpack(l.beta[n + U1]));
-  const float by_label = u + 1 < U1 ? share(l.nodes.label[n], cell_unpack(l.beta[n + 1])) : 0.f;
+  const bool last = t + 1 == l.tb[b], more = u + 1 < U1;
+  const float by_blank = last ? (more ? 0.f : share(arcs.x, arcs.y, Cell{0.5f, 1})) : share(arcs.x, arcs.y, cell_unpack(l.beta[n + U1]));
+  const float by_label = more ? share(arcs.z, arcs.w, cell_unpack(l.beta[n + 1])) : 0.f;
   k.coef[i] = by_blank;
   k.coef[k.R + i] = by_label;
   k.scale[i] = by_blank + by_label;
   k.lse2[i] = l.nodes.lse2[n];
 }
 
-// z = relu(e + p) of a chunk's rows, in panels.
-__global__ __launch_bounds__(256) void lattice_z_kernel(LatticeDev l, LossChunk k, const int2 *from, bf16_t *dst, size_t plane, int blocks, int planes, int vec) {
-  const int live = chunk_rows(k), used = min((live + 255) & ~255, k.R);
-  const size_t total = (size_t)used * blocks * 4;
-  LossPack e{}, p{};
-  e.dtype = p.dtype = l.dtype;
-  e.cols = p.cols = l.H;
-  e.vec = p.vec = vec;
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (size_t)gridDim.x * 256) {
-    const int q = (int)(i & 3);
-    const size_t rest = i >> 2;
-    const int row = (int)(rest % used), blk = (int)(rest / used), c = blk * 32 + q * 8;
-    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (row < live && c < l.H) {
-      const int2 f = from[row];
-      const int b = f.x / l.T, t = f.x - b * l.T, u = f.y - b * (l.U + 1);
-      float y[8];
-      const size_t size = l.dtype ? 2 : 4;
-      e.src = (const char *)l.e + (b * l.e_b + t * l.e_t) * size;
-      p.src = (const char *)l.p + (b * l.p_b + u * l.p_u) * size;
-      loss_load8(e, 0, c, x);
-      loss_load8(p, 0, c, y);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) { x[j] += y[j]; x[j] = x[j] > 0.f || x[j] != x[j] ? x[j] : 0.f; }   // NaN stays
-    }
-    loss_split8(x, planes, dst + (size_t)blk * k.R * 32 + (size_t)row * 32 + q * 8, plane);
+// Sums of dz, where z is above zero, over the chunk's rows of one frame (which = 0) or of one prediction row (which = 1): a workgroup 256 columns,
+// its waves share the rows.  The whole lattice in one chunk: the sums are rounded and stored, rows that no utterance has as zeros.  Else the
+// chunk that holds the first of a sum's rows writes, later ones add, and lattice_done_kernel rounds.
+struct LatticeFold {
+  const float *dz;
+  int ld, splits;
+  size_t part;
+  float *sum[2];               // [B T, ld], [B (U + 1), ld], or null
+  void *out[2];                // the gradients de, dp, or null
+};
+__device__ __forceinline__ f32x4 lattice_load4(const LatticeDev &l, const char *row, int c) {
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  if (l.dtype) {
+    const bf16_t *s = (const bf16_t *)row + c;
+    if (l.vec && c + 4 <= l.H) {
+      const u32x2 w = *reinterpret_cast<const u32x2 *>(s);
+      v = f32x4{__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xFFFF0000u), __uint_as_float(w[1] << 16), __uint_as_float(w[1] & 0xFFFF0000u)};
+    } else
+      for (int j = 0; j < 4; ++j) v[j] = c + j < l.H ? bf16_bits_to_f32(s[j]) : 0.f;
+  } else {
+    const float *s = (const float *)row + c;
+    if (l.vec && c + 4 <= l.H) v = *reinterpret_cast<const f32x4 *>(s);
+    else
+      for (int j = 0; j < 4; ++j) v[j] = c + j < l.H ? s[j] : 0.f;
+  }
+  return v;
+}
+__device__ __forceinline__ void lattice_store4(const LatticeDev &l, void *out, size_t row, int c, f32x4 v) {
+  for (int j = 0; j < 4 && c + j < l.H; ++j) {
+    if (l.dtype) ((bf16_t *)out)[row * l.H + c + j] = (bf16_t)f32_to_bf16_bits(v[j]);
+    else ((float *)out)[row * l.H + c + j] = v[j];
   }
 }
-
-// Sums of dz over the chunk's rows of one frame (which = 0) or of one prediction row (which = 1): a workgroup 256 columns, its waves share the rows.
-// The chunk that holds the first of them writes, later ones add.
-__global__ __launch_bounds__(256) void lattice_fold_kernel(LatticeDev l, LossChunk k, const float *dz, int ld, int which, float *out) {
+__device__ __forceinline__ void lattice_fold(const LatticeDev &l, const LossChunk &k, const LatticeFold &f, int which, int block) {
   __shared__ f32x4 sums[4][64];
-  const int live = chunk_rows(k), per = which ? l.U + 1 : l.T;
-  const int b = blockIdx.x / per, x = blockIdx.x - b * per;
+  const int across = (f.ld + 255) / 256, row = block / across, per = which ? l.U + 1 : l.T;
+  const int live = chunk_rows(k), b = row / per, x = row - b * per;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (block - row * across) * 256 + lane * 4;
   const int T = l.tb[b], U1 = l.ub[b] + 1;
-  if (T == 0 || x >= (which ? U1 : T)) return;
+  const bool whole = f.sum[which] == nullptr;
+  if (T == 0 || x >= (which ? U1 : T)) {
+    if (whole && wave == 0 && c < l.H) lattice_store4(l, f.out[which], row, c, f32x4{0.f, 0.f, 0.f, 0.f});
+    return;
+  }
   // rows first + step * j, j = 0 .. n - 1
   const int first = l.off[b] + (which ? x : x * U1), step = which ? U1 : 1, n = which ? T : U1;
   const int j0 = first >= k.c0 ? 0 : (k.c0 - first + step - 1) / step;
   const int over = k.c0 + live - first;                       // rows below this are in the chunk or before it
   const int j1 = over <= 0 ? 0 : min(n, (over + step - 1) / step);
   if (j0 >= j1) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.y * 256 + lane * 4;
   f32x4 s = {0.f, 0.f, 0.f, 0.f};
-  if (c < ld)
-    for (int j = j0 + wave; j < j1; j += 4) s += *reinterpret_cast<const f32x4 *>(dz + (size_t)(first + j * step - k.c0) * ld + c);
+  if (c < l.H) {
+    const f32x4 own = lattice_load4(l, which ? lattice_p(l, b, x) : lattice_e(l, b, x), c);
+#pragma unroll 4
+    for (int j = j0 + wave; j < j1; j += 4) {
+      const float *at = f.dz + (size_t)(first + j * step - k.c0) * f.ld + c;
+      f32x4 v = *reinterpret_cast<const f32x4 *>(at);
+      const f32x4 other = lattice_load4(l, which ? lattice_e(l, b, j) : lattice_p(l, b, j), c);
+      for (int q = 1; q < f.splits; ++q) v += *reinterpret_cast<const f32x4 *>(at + (size_t)q * f.part);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[i] += own[i] + other[i] > 0.f ? v[i] : 0.f;
+    }
+  }
   sums[wave][lane] = s;
   __syncthreads();
-  if (wave || c >= ld) return;
+  if (wave || c >= l.H) return;
   s = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
-  f32x4 *o = reinterpret_cast<f32x4 *>(out + (size_t)blockIdx.x * ld + c);
+  if (whole) {
+    lattice_store4(l, f.out[which], row, c, s);
+    return;
+  }
+  f32x4 *o = reinterpret_cast<f32x4 *>(f.sum[which] + (size_t)row * f.ld + c);
   *o = j0 > 0 ? *o + s : s;
 }
+// The last launch of a chunk: db, the sums over parts of dW, and what dz gives to encoder and prediction rows.
+__global__ __launch_bounds__(256) void lattice_finish_kernel(LossFinish f, LossChunk k, LatticeDev l, LatticeFold fold, int n_e) {
+  int block = (int)blockIdx.x;
+  if (loss_finish(f, k, block)) return;
+  lattice_fold(l, k, fold, block < n_e ? 0 : 1, block < n_e ? block : block - n_e);
+}
 
-// Rounded once; rows that no utterance has are zero.
-__global__ __launch_bounds__(256) void lattice_fold_done_kernel(LatticeDev l, const float *in, int ld, int which, void *out) {
-  const int per = which ? l.U + 1 : l.T;
-  const size_t total = (size_t)l.B * per * l.H;
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (size_t)gridDim.x * 256) {
-    const size_t row = i / l.H;
-    const int h = (int)(i - row * l.H), b = (int)(row / per), x = (int)(row - (size_t)b * per);
+// The sums of several chunks, rounded once; rows that no utterance has are zero.
+__global__ __launch_bounds__(256) void lattice_done_kernel(LatticeDev l, LatticeFold f) {
+  const int per_row = (l.H + 3) / 4;
+  const size_t rows_e = f.out[0] ? (size_t)l.B * l.T : 0, rows = rows_e + (f.out[1] ? (size_t)l.B * (l.U + 1) : 0);
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < rows * per_row; i += (size_t)gridDim.x * 256) {
+    size_t row = i / per_row;
+    const int c = (int)(i - row * per_row) * 4, which = row >= rows_e;
+    if (which) row -= rows_e;
+    const int per = which ? l.U + 1 : l.T, b = (int)(row / per), x = (int)(row - (size_t)b * per);
     const bool there = l.tb[b] > 0 && x < (which ? l.ub[b] + 1 : l.tb[b]);
-    const float v = there ? in[row * ld + h] : 0.f;
-    if (l.dtype) ((bf16_t *)out)[i] = (bf16_t)f32_to_bf16_bits(v);
-    else ((float *)out)[i] = v;
+    lattice_store4(l, f.out[which], row, c, there ? *reinterpret_cast<const f32x4 *>(f.sum[which] + row * f.ld + c) : f32x4{0.f, 0.f, 0.f, 0.f});
   }
 }
 
