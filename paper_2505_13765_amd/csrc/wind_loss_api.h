@@ -73,14 +73,15 @@ struct LossPlan {
   int kind, dtype, V1, H, K;
   long long N;                       // rows at most
   bool grads;
-  int B, T, U;                       // lattice
+  int B, T, U, cells, skew;          // lattice
+  long long places;
   // derived
   int R, chunks, vblk, hblk, hd, pa, pw, pd;
   LossPick x, z, w;                  // logits, dz, dW
   bool dw_direct, dz_direct;         // written by their products: one chunk and one part; one part
   // offsets into the workspace
   size_t idx, state, count, wp, rows, label, value, coef, scale, lse2, logit, part, dx, colsum, dw, total;
-  size_t off, tb, ub, arcs, nlse2, alpha, beta, dz, de, dp;
+  size_t off, place, tb, ub, slot, arcs, nlse2, alpha, beta, dz, de, dp;
 };
 
 void loss_plan(LossPlan &p) {
@@ -126,7 +127,9 @@ void loss_plan(LossPlan &p) {
     p.off = take(((size_t)p.B + 1) * 4);
     p.tb = take((size_t)p.B * 4);
     p.ub = take((size_t)p.B * 4);
-    p.arcs = take(n * 16);
+    p.place = take((size_t)p.B * 4);
+    p.slot = take(R * 4);
+    p.arcs = take((size_t)p.places * 16);
     p.nlse2 = take(n * 4);
   }
   if (p.grads) {
@@ -135,8 +138,8 @@ void loss_plan(LossPlan &p) {
     p.dw = p.dw_direct ? at : take((size_t)p.w.splits * p.V1 * p.hd * 4);
     p.dz = p.dz_direct ? at : take((size_t)p.z.splits * R * p.hd * 4);
     if (p.kind == kLossLattice) {
-      p.alpha = take(n * 8);
-      p.beta = take(n * 8);
+      p.alpha = take((size_t)p.places * 8);
+      p.beta = take((size_t)p.places * 8);
       if (p.chunks > 1) {
         p.de = take((size_t)p.B * p.T * p.hd * 4);
         p.dp = take((size_t)p.B * (p.U + 1) * p.hd * 4);
@@ -372,6 +375,7 @@ int lattice_plan(LossPlan &p, const wind_output_layer *layer, int B, int T, int 
   if (rc) return rc;
   if (B < 1 || T < 0 || U < 0) return fail(WIND_ERR_ARG, "B >= 1, T >= 0 and U >= 0 required");
   if (U > 4095) return fail(WIND_ERR_UNSUPPORTED, "U must be at most 4095");
+  if ((double)T * (U + 1.0) >= 134217728.0) return fail(WIND_ERR_UNSUPPORTED, "T * (U + 1) must be below 2^27");
   if ((double)B * T * (U + 1.0) >= 2147483648.0 || (double)B * ((double)T + U + 1.0) * ((layer->H + 255) / 256) >= 2147483648.0) return fail(WIND_ERR_UNSUPPORTED, "B * T * (U + 1) and B * (T + U + 1) * H / 256 must be below 2^31");
   p.kind = kLossLattice;
   p.dtype = layer->dtype;
@@ -382,6 +386,10 @@ int lattice_plan(LossPlan &p, const wind_output_layer *layer, int B, int T, int 
   p.T = T;
   p.U = U;
   p.N = (long long)B * T * (U + 1);
+  p.cells = U < 64 ? 1 : U < 128 ? 2 : U < 256 ? 4 : U < 1024 ? 1 : 4;   // of a thread of lattice_sums_kernel
+  p.places = (long long)B * (T + U / p.cells) * (U + 1);
+  p.skew = U <= T && p.places < 1ll << 31;
+  if (!p.skew) p.places = p.N;
   p.grads = grads;
   loss_plan(p);
   return loss_rows_limits(p);
@@ -505,7 +513,10 @@ int wind_transducer_loss(const wind_output_layer *layer, const void *e, int64_t 
   l.tb = r.at<int>(p.tb);
   l.ub = r.at<int>(p.ub);
   l.count = r.at<int>(p.count);
-  l.nodes = LossNodes{r.at<float4>(p.arcs), r.at<float>(p.nlse2)};
+  l.nodes = LossNodes{r.at<float4>(p.arcs), r.at<int>(p.slot), r.at<float>(p.nlse2)};
+  l.place = r.at<int>(p.place);
+  l.cells = p.cells;
+  l.skew = p.skew;
   l.vec = (uintptr_t)e % 16 == 0 && (uintptr_t)p_ % 16 == 0 && e_stride_b % 8 == 0 && e_stride_t % 8 == 0 && p_stride_b % 8 == 0 && p_stride_u % 8 == 0;
   if (p.grads) {
     l.alpha = r.at<float2>(p.alpha);

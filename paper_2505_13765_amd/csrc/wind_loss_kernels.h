@@ -300,7 +300,7 @@ struct LossEntries {
       in[mi] = inside(label[mi][0] - col0) || inside(label[mi][1] - col0);
     }
 #pragma unroll 4
-    for (int e = 2; e < k.K; ++e)
+    for (int e = 2 + ((threadIdx.x & 63) >> 5); e < k.K; e += 2)   // a row's two lanes share them
 #pragma unroll
       for (int mi = 0; mi < T::MI; ++mi) in[mi] |= inside(k.label[(size_t)e * k.R + i0 + 32 * mi] - col0);
     hit = 0;
@@ -308,9 +308,24 @@ struct LossEntries {
     for (int mi = 0; mi < T::MI; ++mi) hit |= __any(in[mi]) ? 1u << mi : 0u;
   }
   static __device__ __forceinline__ bool inside(int at) { return (unsigned)at < (unsigned)(32 * T::NI); }
-  // entry e of the lane's row of block mi
-  __device__ __forceinline__ int at(const LossChunk &k, int e, int mi, int i0) const {
-    return e == 0 ? label[mi][0] : e == 1 ? label[mi][1] : k.label[(size_t)e * k.R + i0 + 32 * mi];
+  // Entries of the lane's row of block mi, from e0 on: eight a lane, the row's two lanes one after the other.  at: column, or anything that is not
+  // inside.  (All of a batch are asked for together: one by one, 64 entries a row cost as much again as the product of fp32 rows of 640.)
+  static constexpr int kBatch = 16;
+  __device__ __forceinline__ void batch(const LossChunk &k, int mi, int i, int e0, int col0, int (&at)[8]) const {
+    const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) at[x] = -1;
+    if (k.K <= 2) {
+      at[0] = label[mi][0] - col0;
+      at[1] = label[mi][1] - col0;
+      if (half) at[0] = at[1] = -1;
+      return;
+    }
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      const int e = e0 + 8 * half + x;
+      if (e < k.K) at[x] = k.label[(size_t)e * k.R + i] - col0;
+    }
   }
 };
 // accumulators that start as the bias; columns past the end as -inf, which exp2 turns into nothing
@@ -363,9 +378,12 @@ __global__ __launch_bounds__(256, T::W) void loss_stats_kernel(LossProduct g, Lo
     if (lane < 32 && col0 < g.cols) k.part[(size_t)(col0 / (32 * T::NI)) * k.R + i] = make_float2(mc, sum);
     if (entries.hit >> mi & 1u) {
       loss_tile_out<T>(acc[mi], tile);
-      for (int e = lane >> 5; e < k.K; e += 2) {   // a row's entries are shared by its two lanes
-        const int at = entries.at(k, e, mi, i0) - col0;
-        if (entries.inside(at)) k.logit[(size_t)e * k.R + i] = tile[(lane & 31) * T::PITCH + at];
+      for (int e0 = 0; e0 < k.K; e0 += entries.kBatch) {
+        int at[8];
+        entries.batch(k, mi, i, e0, col0, at);
+#pragma unroll
+        for (int x = 0; x < 8; ++x)
+          if (entries.inside(at[x])) k.logit[(size_t)(e0 + 8 * (lane >> 5) + x) * k.R + i] = tile[(lane & 31) * T::PITCH + at[x]];
       }
       __builtin_amdgcn_wave_barrier();
     }
@@ -382,8 +400,9 @@ __device__ __forceinline__ Cell cell_of_log2(float l) {   // 2^l, 1 <= m < 2
   return Cell{__builtin_amdgcn_exp2f(l - f), (int)f};
 }
 struct LossNodes {
-  float4 *arcs;                // per lattice node: the probabilities of blank and of its label (m, e, m, e; e as bits)
-  float *lse2;
+  float4 *arcs;                // per place of a lattice node: the probabilities of blank and of its label (m, e, m, e; e as bits)
+  int *slot;                   // [R] places of the chunk's nodes
+  float *lse2;                 // per node
 };
 __global__ __launch_bounds__(256) void loss_rows_done_kernel(LossRowsDev r, LossChunk k, int parts, LossNodes nodes) {
   __shared__ float sm[16][16], ss[16][16];
@@ -403,7 +422,6 @@ __global__ __launch_bounds__(256) void loss_rows_done_kernel(LossRowsDev r, Loss
   sm[grp][lane] = m;
   ss[grp][lane] = s;
   __syncthreads();
-  if (grp || i >= live) return;
   float top = sm[0][lane];
 #pragma unroll
   for (int q = 1; q < 16; ++q) top = fmaxf(top, sm[q][lane]);
@@ -411,28 +429,36 @@ __global__ __launch_bounds__(256) void loss_rows_done_kernel(LossRowsDev r, Loss
   s = 0.f;
 #pragma unroll
   for (int q = 0; q < 16; ++q) s += ss[q][lane] * __builtin_amdgcn_exp2f(sm[q][lane] - ref);
-  const float ls = log2f(s), lse2 = top + ls;
-  k.lse2[i] = lse2;
+  const float ls = log2f(s);
+  // -log2 p of entry e
+  auto cost = [&](int e) { return __builtin_fmaf(-k.logit[(size_t)e * k.R + i], k.c, top) + ls; };
+  if (grp == 0 && i < live) k.lse2[i] = top + ls;
   if (r.kind == kLossLattice) {
-    const int n = k.c0 + i;
-    nodes.lse2[n] = lse2;
-    const Cell stay = cell_of_log2(-(__builtin_fmaf(-k.logit[i], k.c, top) + ls));
-    const Cell take = cell_of_log2(k.label[(size_t)k.R + i] < 0 ? -__builtin_inff() : -(__builtin_fmaf(-k.logit[(size_t)k.R + i], k.c, top) + ls));
-    nodes.arcs[n] = make_float4(stay.m, __int_as_float(stay.e), take.m, __int_as_float(take.e));
+    if (grp || i >= live) return;
+    const Cell stay = cell_of_log2(-cost(0)), take = cell_of_log2(k.label[(size_t)k.R + i] < 0 ? -__builtin_inff() : -cost(1));
+    nodes.lse2[k.c0 + i] = top + ls;
+    nodes.arcs[nodes.slot[i]] = make_float4(stay.m, __int_as_float(stay.e), take.m, __int_as_float(take.e));
     return;
   }
-  const int n = r.idx[k.c0 + i];
   if (r.kind == kLossLabel) {
-    r.loss[n] = (__builtin_fmaf(-k.logit[i], k.c, top) + ls) * (float)kLn2;
+    if (grp == 0 && i < live) r.loss[r.idx[k.c0 + i]] = cost(0) * (float)kLn2;
     return;
   }
   float sum = 0.f;
-  for (int e = 0; e < k.K; ++e) {
-    if (k.label[(size_t)e * k.R + i] < 0) continue;
-    const float lq = k.value[(size_t)e * k.R + i], q = exp2f(lq);
-    if (q != 0.f) sum += q * (lq + (__builtin_fmaf(-k.logit[(size_t)e * k.R + i], k.c, top) + ls));
+  if (i < live) {
+#pragma unroll 4
+    for (int e = grp; e < k.K; e += 16) {
+      const float lq = k.value[(size_t)e * k.R + i], q = exp2f(lq);   // (an entry that is not there has q = 0)
+      if (q != 0.f) sum += q * (lq + cost(e));
+    }
   }
-  r.loss[n] = sum * (float)kLn2 * r.tau * r.tau;
+  __syncthreads();
+  sm[grp][lane] = sum;
+  __syncthreads();
+  if (grp || i >= live) return;
+#pragma unroll
+  for (int q = 1; q < 16; ++q) sum += sm[q][lane];
+  r.loss[r.idx[k.c0 + i]] = sum * (float)kLn2 * r.tau * r.tau;
 }
 
 // dx of a chunk, in panels, and its column sums.
@@ -470,13 +496,23 @@ __global__ __launch_bounds__(256, T::W) void loss_dx_kernel(LossProduct g, LossC
     if (entries.hit >> mi & 1u) {
       loss_tile_out<T>(acc[mi], tile);
       float *row = tile + (lane & 31) * T::PITCH;
-      if (lane < 32)   // one lane a row: an output that is named twice is taken off twice, in order
-        for (int e = 0; e < k.K; ++e) {
-          const int at = entries.at(k, e, mi, i0) - col0;
-          if (entries.inside(at)) row[at] -= k.coef[(size_t)e * k.R + i];
+      for (int e0 = 0; e0 < k.K; e0 += entries.kBatch) {
+        int at[8];
+        float c[8];
+        entries.batch(k, mi, i, e0, col0, at);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) c[x] = e0 + 8 * half + x < k.K ? k.coef[(size_t)(e0 + 8 * half + x) * k.R + i] : 0.f;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {   // one lane of a row after the other: an output that is named twice is taken off twice, in order
+          if (half == h) {
+#pragma unroll
+            for (int x = 0; x < 8; ++x)
+              if (entries.inside(at[x])) row[at[x]] -= c[x];
+          }
+          __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+          __builtin_amdgcn_wave_barrier();
         }
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
+      }
 #pragma unroll
       for (int ni = 0; ni < T::NI; ++ni)
 #pragma unroll

@@ -4,7 +4,9 @@
 // Node (t, u) of utterance b: u labels emitted, frame t looked at; its row z = relu(e[b, t] + p[b, u]) gives blank (to (t + 1, u)) and label y[u]
 // (to (t, u + 1)) their probabilities.  alpha(t, u) is the probability of reaching it, beta(t, u) of finishing from it, P = beta(0, 0); an arc's
 // expected count is alpha(from) p(arc) beta(to) / P, and these are the scale and the coefficients of the node's row.
-// Only nodes with t < frames[b], u <= counts[b] are rows; they are numbered b by b, t by t.
+// Only nodes with t < frames[b], u <= counts[b] are rows; they are numbered b by b, t by t.  What the recursions read and write (arcs, alpha, beta) lies
+// in another order where there are at least as many frames as labels: diagonal by diagonal of the threads that run them, so that what a wave asks for
+// at a time is consecutive memory (by rows, 64 lanes touch 64 cache lines).
 //
 // Numbers.  A cell is a mantissa and an exponent of its own (m 2^e, 0.5 <= m < 1, e a 32-bit integer).  A step of the recursion is then two
 // products and one addition in fp32, relative error 2^-23 per step however improbable the cell, and no logarithm or exponential on
@@ -22,16 +24,20 @@ struct LatticeDev {
   const int *labels, *frames, *counts;        // [B, U], [B], [B]
   const float *weights;                       // [B] or null
   float *loss;                                // [B]
-  int *tb, *ub, *off, *count;                 // frames (0: left out) and labels as they are used, first row, rows in all
+  int *tb, *ub, *off, *place, *count;         // frames (0: left out) and labels as they are used, first row, first place, rows in all
+  int cells, skew;                            // cells of a thread; 1: places lie diagonal by diagonal
   LossNodes nodes;
-  float2 *alpha, *beta;                       // per node: mantissa, exponent (int bits)
+  float2 *alpha, *beta;                       // per place: mantissa, exponent (int bits)
 };
+// places of T frames of U1 nodes; that of node (0, u), from which those of the later frames follow U1 apart
+__device__ __forceinline__ int lattice_places(const LatticeDev &l, int T, int U1) { return T ? (T + (l.skew ? (U1 - 1) / l.cells : 0)) * U1 : 0; }
+__device__ __forceinline__ int lattice_place(const LatticeDev &l, int first, int U1, int u) { return first + u + (l.skew ? u / l.cells * U1 : 0); }
 __device__ __forceinline__ const char *lattice_e(const LatticeDev &l, int b, int t) { return (const char *)l.e + (b * l.e_b + t * l.e_t) * (l.dtype ? 2 : 4); }
 __device__ __forceinline__ const char *lattice_p(const LatticeDev &l, int b, int u) { return (const char *)l.p + (b * l.p_b + u * l.p_u) * (l.dtype ? 2 : 4); }
 
 // One workgroup: which utterances count, and where their rows begin.
 __device__ __forceinline__ void lattice_rows(const LatticeDev &l) {
-  __shared__ int wave_sum_[4], total_;
+  __shared__ int wave_sum_[2][4], total_[2];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   for (int b = wave; b < l.B; b += 4) {
     const int T = min(max(l.frames[b], 0), l.T), U = min(max(l.counts[b], 0), l.U);
@@ -47,28 +53,41 @@ __device__ __forceinline__ void lattice_rows(const LatticeDev &l) {
       if (wrong || T == 0) l.loss[b] = wrong ? __builtin_nanf("") : 0.f;
     }
   }
-  if (tid == 0) total_ = 0;
+  if (tid < 2) total_[tid] = 0;
   __syncthreads();
   for (int base = 0; base < l.B; base += 256) {
     const int b = base + tid;
-    const int n = b < l.B ? l.tb[b] * (l.ub[b] + 1) : 0;
-    int sum = n;
-    for (int d = 1; d < 64; d <<= 1) {
-      const int o = __shfl_up(sum, d);
-      if (lane >= d) sum += o;
+    int n[2] = {0, 0}, sum[2], at[2];
+    if (b < l.B) {
+      n[0] = l.tb[b] * (l.ub[b] + 1);
+      n[1] = lattice_places(l, l.tb[b], l.ub[b] + 1);
     }
-    if (lane == 63) wave_sum_[wave] = sum;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      sum[q] = n[q];
+      for (int d = 1; d < 64; d <<= 1) {
+        const int o = __shfl_up(sum[q], d);
+        if (lane >= d) sum[q] += o;
+      }
+      if (lane == 63) wave_sum_[q][wave] = sum[q];
+    }
     __syncthreads();
-    int at = total_;
-    for (int w = 0; w < wave; ++w) at += wave_sum_[w];
-    if (b < l.B) l.off[b] = at + sum - n;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      at[q] = total_[q];
+      for (int w = 0; w < wave; ++w) at[q] += wave_sum_[q][w];
+      if (b < l.B) (q ? l.place : l.off)[b] = at[q] + sum[q] - n[q];
+    }
     __syncthreads();
-    if (tid == 255) total_ = at + sum;
+    if (tid == 255) {
+      total_[0] = at[0] + sum[0];
+      total_[1] = at[1] + sum[1];
+    }
     __syncthreads();
   }
   if (tid == 0) {
-    l.off[l.B] = total_;
-    *l.count = total_;
+    l.off[l.B] = total_[0];
+    *l.count = total_[0];
   }
 }
 // The first launch of a call: the rows, and W into panels.
@@ -87,78 +106,97 @@ __device__ __forceinline__ Cell cell_product(Cell a, Cell b) { return Cell{a.m *
 __device__ __forceinline__ float2 cell_pack(Cell c) { return make_float2(c.m, __int_as_float(c.e)); }
 __device__ __forceinline__ Cell cell_unpack(float2 v) { return Cell{v.x, __float_as_int(v.y)}; }
 
-// One workgroup runs one utterance's recursion, alpha or beta (mirrored: t' = T - 1 - t, u' = U - u), along diagonals: thread i owns C
+// One workgroup runs one utterance's recursion, alpha (FWD) or beta (mirrored: t' = T - 1 - t, u' = U - u), along diagonals: thread i owns C
 // consecutive u, is one frame behind thread i - 1, and takes what its neighbour's last cell hands on from the lane before it, or, in a
 // workgroup of several waves (MULTI), from LDS at a wave's edge.  Cells outside the lattice need no branch: before its first frame a
 // thread's inputs are zero, and what is computed past the last frame or label reaches no cell that counts.  The next AHEAD
 // frames' arcs are on their way while the present ones are worked off.
-// The time is the number of diagonals, T + U / C, times C dependent steps of about 40 cycles and their issue: 750 frames and 120 labels
-// (C = 2) ran 529 us with logarithms converted on the way, a barrier and LDS per diagonal.
-template <int C, int AHEAD, bool MULTI>
-__global__ __launch_bounds__(MULTI ? 1024 : 64) void lattice_sums_kernel(LatticeDev l, int both) {
-  __shared__ float2 edge[2][17];
-  const int b = both ? (int)blockIdx.x >> 1 : (int)blockIdx.x;
-  const bool fwd = both && (blockIdx.x & 1);
-  const int T = l.tb[b], U1 = l.ub[b] + 1, off = l.off[b], tid = threadIdx.x, wave = tid >> 6;
-  if (T == 0) return;
-  const int lanes = (U1 + C - 1) / C, steps = T + lanes - 1;
-  // this thread's nodes: cell (t', u' = tid C + j)
-  auto node = [&](int t, int j) {
-    const int u = min(tid * C + j, U1 - 1), tc = min(max(t, 0), T - 1);
-    return off + (fwd ? tc * U1 + u : (T - 1 - tc) * U1 + (U1 - 1 - u));
-  };
-  Cell up[C], out{0.f, kCellZero};       // what comes from the frame before; what the last cell hands on
+// The time is the number of diagonals, T + U / C, times C dependent steps and their issue by one wave.
+template <int C, int AHEAD, bool MULTI, bool FWD>
+__device__ __forceinline__ void lattice_run(const LatticeDev &l, int b, bool keep, float2 (&edge)[2][17]) {
+  const int T = l.tb[b], U1 = l.ub[b] + 1, first = l.place[b], tid = threadIdx.x, wave = tid >> 6;
+  const int steps = T + (U1 + C - 1) / C - 1;
+  const char *const arcs_at = (const char *)(l.nodes.arcs + first);
+  char *const keep_at = (char *)((FWD ? l.alpha : l.beta) + first);
+  // byte offsets of this thread's nodes, cells (t', u' = tid C + j), for the next arcs to ask for and for the present cell (half as far)
+  uint32_t ask[C], put[C];
+  bool mine[C];
+#pragma unroll
+  for (int j = 0; j < C; ++j) {
+    const int u = min(tid * C + j, U1 - 1);
+    mine[j] = tid * C + j < U1;
+    ask[j] = (uint32_t)(lattice_place(l, 0, U1, FWD ? u : U1 - 1 - u) + (FWD ? 0 : (T - 1) * U1)) * 16u;
+    put[j] = ask[j] / 2;
+  }
+  const uint32_t row = (uint32_t)U1 * 16u;
+  int t_ask = -tid, t = -tid;
+  Cell up[C], out{0.f, kCellZero}, last{0.f, kCellZero};   // what comes from the frame before; what the last cell hands on; beta(0, 0)
 #pragma unroll
   for (int j = 0; j < C; ++j) up[j] = (tid == 0 && j == 0) ? Cell{0.5f, 1} : Cell{0.f, kCellZero};
   float4 arcs[2][AHEAD][C];
-  auto request = [&](int set, int d0) {
+  auto request = [&](int set) {
 #pragma unroll
-    for (int s = 0; s < AHEAD; ++s)
+    for (int s = 0; s < AHEAD; ++s) {
 #pragma unroll
-      for (int j = 0; j < C; ++j) arcs[set][s][j] = l.nodes.arcs[node(d0 + s - tid, j)];
+      for (int j = 0; j < C; ++j) arcs[set][s][j] = *reinterpret_cast<const float4 *>(arcs_at + ask[j]);
+      const uint32_t step = (unsigned)t_ask++ < (unsigned)(T - 1) ? row : 0u;   // stays on the first and on the last frame
+#pragma unroll
+      for (int j = 0; j < C; ++j) ask[j] = FWD ? ask[j] + step : ask[j] - step;
+    }
   };
   auto work = [&](int set, int d0) {
 #pragma unroll
     for (int s = 0; s < AHEAD; ++s) {
-      const int d = d0 + s, t = d - tid;
-      // the neighbour's, one diagonal ago
-      Cell left;
+      Cell left;                          // the neighbour's, one diagonal ago
       left.m = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, out.m), 0x138, 0xF, 0xF, false));
       left.e = __builtin_amdgcn_update_dpp(kCellZero, out.e, 0x138, 0xF, 0xF, false);
       if (MULTI) {
-        if ((tid & 63) == 63) edge[d & 1][wave + 1] = cell_pack(out);
+        const int d = (d0 + s) & 1;
+        if ((tid & 63) == 63) edge[d][wave + 1] = cell_pack(out);
         __syncthreads();
-        if ((tid & 63) == 0) left = cell_unpack(edge[d & 1][wave]);
+        if ((tid & 63) == 0) left = cell_unpack(edge[d][wave]);
       }
+      const bool here = (unsigned)t < (unsigned)T;
 #pragma unroll
       for (int j = 0; j < C; ++j) {
         const float4 a = arcs[set][s][j];
         const Cell stay{a.x, __float_as_int(a.y)}, take{a.z, __float_as_int(a.w)};
         Cell v;
-        if (fwd) {                        // hands on what its own arcs make of it
+        if (FWD) {                        // hands on what its own arcs make of it
           v = cell_sum(up[j], left);
           up[j] = cell_product(v, stay);
           left = cell_product(v, take);
         } else {                          // its own arcs make it of what it is handed
           v = cell_sum(cell_product(up[j], stay), cell_product(left, take));
           up[j] = left = v;
+          if (t == T - 1 && tid * C + j == U1 - 1) last = v;
         }
-        const bool here = t >= 0 && t < T && tid * C + j < U1;
-        if (here && both) (fwd ? l.alpha : l.beta)[node(t, j)] = cell_pack(v);
-        if (here && !fwd && t == T - 1 && tid * C + j == U1 - 1) l.loss[b] = (float)(-(log2((double)v.m) + (double)v.e) * kLn2);
+        if (keep && here && mine[j]) *reinterpret_cast<float2 *>(keep_at + put[j]) = cell_pack(v);
       }
       out = left;
+      const uint32_t step = (unsigned)t++ < (unsigned)(T - 1) ? row / 2 : 0u;
+#pragma unroll
+      for (int j = 0; j < C; ++j) put[j] = FWD ? put[j] + step : put[j] - step;
     }
   };
   if (MULTI && tid < 34) edge[tid & 1][tid >> 1] = make_float2(0.f, __int_as_float(kCellZero));
-  request(0, 0);
+  request(0);
   if (MULTI) __syncthreads();
   for (int d0 = 0; d0 < steps; d0 += 2 * AHEAD) {
-    request(1, d0 + AHEAD);
+    request(1);
     work(0, d0);
-    request(0, d0 + 2 * AHEAD);
+    request(0);
     work(1, d0 + AHEAD);
   }
+  if (!FWD && tid == (U1 - 1) / C) l.loss[b] = (float)(-(log2((double)last.m) + (double)last.e) * kLn2);
+}
+template <int C, int AHEAD, bool MULTI>
+__global__ __launch_bounds__(MULTI ? 1024 : 64) void lattice_sums_kernel(LatticeDev l, int both) {
+  __shared__ float2 edge[2][17];
+  const int b = both ? (int)blockIdx.x >> 1 : (int)blockIdx.x;
+  if (l.tb[b] == 0) return;
+  if (both && (blockIdx.x & 1)) lattice_run<C, AHEAD, MULTI, true>(l, b, true, edge);
+  else lattice_run<C, AHEAD, MULTI, false>(l, b, both, edge);
 }
 
 // The first launch of a chunk: its rows z = relu(e + p) in panels, their two entries (0: blank, 1: the next label), and for the gradient
@@ -205,18 +243,20 @@ __global__ __launch_bounds__(256) void lattice_chunk_kernel(LatticeDev l, LossCh
     loss_split8(x, planes, to + (size_t)blk * k.R * 32, plane);
   }
   if (q || blockIdx.y) return;
+  const int place = lattice_place(l, l.place[b], U1, u) + t * U1;
+  l.nodes.slot[i] = place;
   k.label[i] = l.V1 - 1;
   k.label[k.R + i] = u + 1 < U1 ? l.labels[(size_t)b * l.U + u] : -1;
   if (!grad) return;
-  const Cell P = cell_unpack(l.beta[l.off[b]]), a = cell_unpack(l.alpha[n]);
-  const float4 arcs = l.nodes.arcs[n];
+  const Cell P = cell_unpack(l.beta[l.place[b]]), a = cell_unpack(l.alpha[place]);
+  const float4 arcs = l.nodes.arcs[place];
   const float w = l.weights ? l.weights[b] : 1.f;
   auto share = [&](float m, float e_bits, Cell next) {   // expected count of an arc, times the utterance's weight
     return P.m == 0.f ? 0.f : w * __builtin_amdgcn_ldexpf(a.m * m * next.m / P.m, a.e + __float_as_int(e_bits) + next.e - P.e);
   };
   const bool last = t + 1 == l.tb[b], more = u + 1 < U1;
-  const float by_blank = last ? (more ? 0.f : share(arcs.x, arcs.y, Cell{0.5f, 1})) : share(arcs.x, arcs.y, cell_unpack(l.beta[n + U1]));
-  const float by_label = more ? share(arcs.z, arcs.w, cell_unpack(l.beta[n + 1])) : 0.f;
+  const float by_blank = last ? (more ? 0.f : share(arcs.x, arcs.y, Cell{0.5f, 1})) : share(arcs.x, arcs.y, cell_unpack(l.beta[place + U1]));
+  const float by_label = more ? share(arcs.z, arcs.w, cell_unpack(l.beta[lattice_place(l, l.place[b], U1, u + 1) + t * U1])) : 0.f;
   k.coef[i] = by_blank;
   k.coef[k.R + i] = by_label;
   k.scale[i] = by_blank + by_label;
