@@ -5,12 +5,12 @@
 namespace {
 
 // Tiles of the products.  rate: of a full chip of them, in parts of kLossRate, for logits and for the products of dx; alone: the part of that left when a CU has one workgroup of them
-// instead of two.  256 x 128 outputs in two workgroups per CU against 256 x 256 in one, sums over 640: 34 us instead of 50 for 5700 rows
+// instead of two; start: a tile's start and results, in slabs.  256 x 128 outputs in two workgroups per CU against 256 x 256 in one, sums over 640: 34 us instead of 50 for 5700 rows
 // and 4097 outputs (one's start and results behind the other's products), 1 to 5 % less over 2048; the products of dx, whose sums are
 // longer and whose results cost less: 1.51 ms in one workgroup of 256 x 256, 1.86 in two of 256 x 128 (7373 x 2048 over 65537).
-struct LossShape { int bm, bn; double rate, rate_dx, alone; };
-constexpr LossShape kLossShapes[] = {{256, 256, 0.9, 1.15, 1.0}, {256, 128, 1.0, 1.0, 0.65}, {128, 128, 0.87, 0.87, 0.55}, {64, 64, 0.35, 0.35, 1.0}};
-constexpr LossShape kLossShapesF32[] = {{128, 128, 0.75, 0.75, 1.0}, {64, 64, 0.6, 0.6, 0.65}};
+struct LossShape { int bm, bn; double rate, rate_dx, alone, start; };
+constexpr LossShape kLossShapes[] = {{256, 256, 0.9, 1.15, 1.0, 12}, {256, 128, 1.0, 1.0, 0.65, 6}, {128, 128, 0.87, 0.87, 0.55, 6}, {64, 64, 0.35, 0.35, 1.0, 8}};
+constexpr LossShape kLossShapesF32[] = {{128, 128, 0.75, 0.75, 1.0, 12}, {64, 64, 0.6, 0.6, 0.65, 8}};
 constexpr double kLossRate = 1.2e15 / 256 / 1e6;   // operations per microsecond and CU
 // the tile of each shape for operands of PA and PB planes
 template <int PA, int PB>
@@ -37,8 +37,12 @@ struct LossTiles<3, 3> {
 
 // dx and rows of a chunk, about.  A chunk of 2700 rows of 65537 outputs (512 MB) left the products of few tiles: 8.9 ms for 7373 rows,
 // one chunk 7.4
-constexpr size_t kLossChunkBytes = 1280u << 20;
+constexpr size_t kLossChunkBytes = 1200u << 20;
 constexpr int kLossMaxEntries = 1024;
+// Entries (of all rows) and column blocks up to which a row tile's last workgroup joins its column blocks: one launch less, 36 -> 31 us for 16 rows of 1025
+// outputs.  With more, that workgroup is what the others' results wait for (3001 rows of 64 entries: 73 us against 51 and 6).
+constexpr long long kLossJoinEntries = 4096;
+constexpr int kLossJoinParts = 128;
 
 // the bf16 planes that make up a stored value of each type, and the sum of two bf16 values (hidden rows of the lattice)
 int loss_planes(int dtype) { return dtype == WIND_BF16 ? 1 : 3; }
@@ -46,7 +50,7 @@ int lattice_planes(int dtype) { return dtype == WIND_BF16 ? 2 : 3; }
 
 struct LossPick { int shape, splits, bm, bn; };
 // Shape, and parts of the summed axis, of a product of m x n outputs over `slabs` slabs of 32: the least time of the fullest CU, where a tile costs
-// its operations and about six slabs for its start and its results, and parts cost the writing and reading of their sums.
+// its operations, its start and its results, and parts cost the writing and reading of their sums.
 LossPick loss_pick(int planes, long long m, long long n, long long slabs, bool split) {
   const LossShape *shapes = planes == 3 ? kLossShapesF32 : kLossShapes;
   const int count = planes == 3 ? 2 : 4, products = planes == 3 ? 6 : planes;
@@ -58,7 +62,7 @@ LossPick loss_pick(int planes, long long m, long long n, long long slabs, bool s
     for (int parts = 1; parts <= (split ? 64 : 1); ++parts) {
       if (parts > 1 && (slabs / parts < 8 || tiles * parts > 1024)) break;
       const long long fullest = (tiles * parts + 255) / 256;
-      const double tile = ((double)((slabs + parts - 1) / parts) * products + 6) * s.bm * s.bn * 64 / (kLossRate * (split ? s.rate_dx : s.rate) * (fullest == 1 ? s.alone : 1.0));
+      const double tile = ((double)((slabs + parts - 1) / parts) * products + s.start) * s.bm * s.bn * 64 / (kLossRate * (split ? s.rate_dx : s.rate) * (fullest == 1 ? s.alone : 1.0));
       const double time = fullest * tile + (parts > 1 ? 1.0 + parts * (double)m * n * 8 / 4e6 : 0.0);
       if (time < least) {
         least = time;
@@ -79,8 +83,10 @@ struct LossPlan {
   int R, chunks, vblk, hblk, hd, pa, pw, pd;
   LossPick x, z, w;                  // logits, dz, dW
   bool dw_direct, dz_direct;         // written by their products: one chunk and one part; one part
+  int parts;                         // column blocks of a row
+  bool join;                         // joined by the launch that makes them
   // offsets into the workspace
-  size_t idx, state, count, wp, rows, label, value, coef, scale, lse2, logit, part, dx, colsum, dw, total;
+  size_t idx, state, count, ticket, wp, rows, label, value, coef, scale, lse2, logit, part, dx, colsum, dw, total;
   size_t off, place, tb, ub, slot, arcs, nlse2, alpha, beta, dz, de, dp;
 };
 
@@ -100,6 +106,8 @@ void loss_plan(LossPlan &p) {
   p.x = loss_pick(p.pa, m, p.V1, p.hblk, false);
   p.z = loss_pick(p.pd, m, p.H, p.vblk, true);
   p.w = loss_pick(p.pd, p.V1, p.H, (m + 31) / 32, true);
+  p.parts = (p.V1 + p.x.bn / 2 - 1) / (p.x.bn / 2);
+  p.join = N * p.K <= kLossJoinEntries && p.parts <= kLossJoinParts;
   p.dw_direct = p.chunks == 1 && p.w.splits == 1;
   p.dz_direct = p.kind != kLossLattice && p.z.splits == 1;
   size_t at = 0;
@@ -110,6 +118,7 @@ void loss_plan(LossPlan &p) {
   };
   const size_t R = (size_t)p.R, n = (size_t)N;
   p.count = take(4);
+  p.ticket = take((size_t)p.R / 64 * 4);
   p.wp = take((size_t)p.pw * p.vblk * 32 * p.hblk * 64);
   p.rows = take((size_t)p.pa * R * p.hblk * 64);
   p.label = take(R * p.K * 4);
@@ -117,7 +126,7 @@ void loss_plan(LossPlan &p) {
   p.coef = take(R * p.K * 4);
   p.scale = take(R * 4);
   p.lse2 = take(R * 4);
-  p.part = take(R * 8 * ((p.V1 + p.x.bn / 2 - 1) / (p.x.bn / 2)));
+  p.part = take(R * 8 * p.parts);
   if (p.kind != kLossLattice) {
     p.idx = take(n * 4);
     p.state = take(n);
@@ -242,7 +251,6 @@ LossPack loss_begin(LossRun &r) {
   w.dst_rows = p.vblk * 32;
   w.blocks = p.hblk;
   w.planes = p.pw;
-  w.vec = (uintptr_t)l.w % 16 == 0 && l.w_stride % 8 == 0;
   return w;
 }
 
@@ -250,11 +258,16 @@ LossProduct loss_logits(const LossRun &r) { return LossProduct{r.x, r.w, r.p.hbl
 void loss_stats(const LossRun &r, LossNodes nodes) {
   const LossPlan &p = r.p;
   const LossProduct g = loss_logits(r);
+  unsigned *ticket = r.at<unsigned>(p.ticket);
   loss_with_tile(p.pa, p.x.shape, [&](auto t) {
     using T = decltype(t);
-    loss_stats_kernel<T><<<loss_grid((p.R + T::BM - 1) / T::BM, g.ct), 256, 0, r.s>>>(g, r.chunk, r.layer->b);
+    const unsigned grid = loss_grid((p.R + T::BM - 1) / T::BM, g.ct);
+    if (p.join) loss_stats_kernel<T, true><<<grid, 256, 0, r.s>>>(g, r.chunk, r.layer->b, r.rows, nodes, ticket);
+    else loss_stats_kernel<T, false><<<grid, 256, 0, r.s>>>(g, r.chunk, r.layer->b, r.rows, nodes, ticket);
   });
-  loss_rows_done_kernel<<<p.R / 16, 256, 0, r.s>>>(r.rows, r.chunk, (p.V1 + p.x.bn / 2 - 1) / (p.x.bn / 2), nodes);
+  if (p.join) return;
+  if (p.parts > 256 && p.R <= 4096) loss_rows_done_kernel<4><<<p.R / 4, 256, 0, r.s>>>(r.rows, r.chunk, p.parts, nodes);
+  else loss_rows_done_kernel<16><<<p.R / 16, 256, 0, r.s>>>(r.rows, r.chunk, p.parts, nodes);
 }
 // dx and its products; what the chunk's last launch has to do then.  dz: the output of one part (label and distillation rows).
 LossFinish loss_gradients(const LossRun &r, int chunk, bool dz, LossOut dz_out, void *dw, float *db) {
@@ -271,35 +284,32 @@ LossFinish loss_gradients(const LossRun &r, int chunk, bool dz, LossOut dz_out, 
     f.n_db = (p.V1 + 15) / 16;
   }
   const PanelsDev dx{d.dx, d.plane, (uint32_t)p.R, (uint32_t)p.vblk};
-  if (dz) {
-    LossOut o = dz_out;
-    if (!p.dz_direct) {
-      o = LossOut{r.at<float>(p.dz), (size_t)p.hd, 0, p.H, 1, nullptr, 0, p.z.splits, (size_t)p.R * p.hd};
-      if (p.kind != kLossLattice) {
-        f.dz = LossJoin{r.at<float>(p.dz), p.z.splits, o.part, o.ld, 0, p.H, p.dtype, dz_out.vec, dz_out.idx, dz_out.p};
-        f.n_dz = (int)loss_blocks((size_t)p.R * (p.hd / 4), 256, 1024);
-      }
+  LossOut zo = dz_out, wo{};
+  if (dz && !p.dz_direct) {
+    zo = LossOut{r.at<float>(p.dz), (size_t)p.hd, 0, p.H, nullptr, 0, p.z.splits, (size_t)p.R * p.hd};
+    if (p.kind != kLossLattice) {
+      f.dz = LossJoin{r.at<float>(p.dz), p.z.splits, zo.part, zo.ld, 0, p.H, p.dtype, dz_out.idx, dz_out.p};
+      f.n_dz = (int)loss_blocks((size_t)p.R * (p.hd / 4), 256, 1024);
     }
-    const LossProduct q{dx, r.w, p.vblk, p.H, (p.H + p.z.bn - 1) / p.z.bn};
-    loss_with_dx_tile(p.pd, p.z.shape, [&](auto t) {
-      using T = decltype(t);
-      loss_dz_kernel<T><<<loss_grid((p.R + T::BM - 1) / T::BM, q.ct, o.splits), 256, 0, r.s>>>(q, r.chunk, o);
-    });
   }
   if (dw) {
-    const LossProduct q{dx, r.x, 0, p.V1, (p.H + p.w.bn - 1) / p.w.bn};
-    const int vec = (uintptr_t)dw % 16 == 0 && p.H % 4 == 0;
-    LossOut o{r.at<float>(p.dw), (size_t)p.hd, 0, p.H, 1, nullptr, chunk > 0, p.w.splits, (size_t)p.V1 * p.hd};
-    if (p.dw_direct) o = LossOut{dw, (size_t)p.H, p.dtype, p.H, vec, nullptr, 0, 1, 0};
+    wo = LossOut{r.at<float>(p.dw), (size_t)p.hd, 0, p.H, nullptr, chunk > 0, p.w.splits, (size_t)p.V1 * p.hd};
+    if (p.dw_direct) wo = LossOut{dw, (size_t)p.H, p.dtype, p.H, nullptr, 0, 1, 0};
     else if (chunk + 1 == p.chunks) {
-      f.dw = LossJoin{r.at<float>(p.dw), p.w.splits, o.part, o.ld, p.V1, p.H, p.dtype, vec, nullptr, dw};
+      f.dw = LossJoin{r.at<float>(p.dw), p.w.splits, wo.part, wo.ld, p.V1, p.H, p.dtype, nullptr, dw};
       f.n_dw = (int)loss_blocks((size_t)p.V1 * (p.hd / 4), 256, 2048);
     }
-    loss_with_dx_tile(p.pd, p.w.shape, [&](auto t) {
-      using T = decltype(t);
-      loss_dw_kernel<T><<<loss_grid((p.V1 + T::BM - 1) / T::BM, q.ct, o.splits), 256, 0, r.s>>>(q, r.chunk, o);
-    });
   }
+  const LossProduct z{dx, r.w, p.vblk, p.H, (p.H + p.z.bn - 1) / p.z.bn}, w{dx, r.x, 0, p.V1, (p.H + p.w.bn - 1) / p.w.bn};
+  const unsigned z_blocks = loss_grid((p.R + p.z.bm - 1) / p.z.bm, z.ct, zo.splits), w_blocks = loss_grid((p.V1 + p.w.bm - 1) / p.w.bm, w.ct, wo.splits);
+  if (dz && dw && p.z.shape == p.w.shape) {
+    loss_with_dx_tile(p.pd, p.z.shape, [&](auto t) {
+      loss_products_kernel<decltype(t)><<<z_blocks + w_blocks, 256, 0, r.s>>>(z, zo, (int)z_blocks, w, wo, r.chunk);
+    });
+    return f;
+  }
+  if (dz) loss_with_dx_tile(p.pd, p.z.shape, [&](auto t) { loss_dz_kernel<decltype(t)><<<z_blocks, 256, 0, r.s>>>(z, r.chunk, zo); });
+  if (dw) loss_with_dx_tile(p.pd, p.w.shape, [&](auto t) { loss_dw_kernel<decltype(t)><<<w_blocks, 256, 0, r.s>>>(w, r.chunk, wo); });
   return f;
 }
 
@@ -328,9 +338,7 @@ int loss_rows_call(const char *name, const wind_output_layer *layer, const void 
   rows.state = r.at<unsigned char>(p.state);
   r.rows = rows;
   const LossPack w = loss_begin(r);
-  const unsigned w_blocks = loss_blocks((size_t)w.dst_rows * p.hblk * 4), states = loss_blocks((size_t)N * std::min(p.K, 64), 256, 1024);
-  loss_begin_kernel<<<w_blocks + states, 256, 0, s>>>(w, (int)w_blocks, rows, dh);
-  loss_compact_kernel<<<1, 1024, 0, s>>>(rows);
+  const unsigned w_blocks = loss_blocks((size_t)w.dst_rows * p.hblk * 4);
   LossPack k{};
   k.src = h;
   k.stride = (size_t)h_stride;
@@ -343,12 +351,20 @@ int loss_rows_call(const char *name, const wind_output_layer *layer, const void 
   k.dst_rows = p.R;
   k.blocks = p.hblk;
   k.planes = p.pa;
-  k.vec = (uintptr_t)h % 16 == 0 && h_stride % 8 == 0;
-  LossOut dz{dh, (size_t)p.H, p.dtype, p.H, dh && (uintptr_t)dh % 16 == 0 && p.H % 4 == 0, nullptr, 0, 1, 0};
+  LossOut dz{dh, (size_t)p.H, p.dtype, p.H, nullptr, 0, 1, 0};
+  const bool small = p.chunks == 1 && N <= kLossSmallRows && N * p.K <= kLossSmall;
+  if (small) {
+    const unsigned across = std::min<unsigned>((unsigned)p.hblk, std::max(1u, 512u / (unsigned)(p.R / 64)));
+    loss_small_kernel<<<w_blocks + (unsigned)(p.R / 64) * across, 256, 0, s>>>(w, (int)w_blocks, rows, k, r.chunk, (int)across, dh, r.at<unsigned>(p.ticket), p.R / 64);
+  } else {
+    const unsigned states = loss_blocks((size_t)N * std::min(p.K, 64), 256, 1024);
+    loss_begin_kernel<<<w_blocks + states, 256, 0, s>>>(w, (int)w_blocks, rows, dh);
+    loss_compact_kernel<<<1, 1024, 0, s>>>(rows, r.at<unsigned>(p.ticket), p.R / 64);
+  }
   for (int c = 0; c < p.chunks; ++c) {
     k.c0 = r.chunk.c0 = c * p.R;
     const unsigned packs = loss_blocks((size_t)p.R * p.hblk * 4), entries = loss_blocks((size_t)p.R * std::min(p.K, 64), 256, 1024);
-    loss_chunk_kernel<<<packs + entries, 256, 0, s>>>(k, (int)packs, rows, r.chunk);
+    if (!small) loss_chunk_kernel<<<packs + entries, 256, 0, s>>>(k, (int)packs, rows, r.chunk);
     loss_stats(r, LossNodes{});
     if (!p.grads) continue;
     dz.idx = rows.idx + k.c0;
@@ -517,21 +533,25 @@ int wind_transducer_loss(const wind_output_layer *layer, const void *e, int64_t 
   l.place = r.at<int>(p.place);
   l.cells = p.cells;
   l.skew = p.skew;
-  l.vec = (uintptr_t)e % 16 == 0 && (uintptr_t)p_ % 16 == 0 && e_stride_b % 8 == 0 && e_stride_t % 8 == 0 && p_stride_b % 8 == 0 && p_stride_u % 8 == 0;
   if (p.grads) {
     l.alpha = r.at<float2>(p.alpha);
     l.beta = r.at<float2>(p.beta);
   }
   const LossPack w = loss_begin(r);
-  lattice_begin_kernel<<<1 + loss_blocks((size_t)w.dst_rows * p.hblk * 4), 256, 0, s>>>(w, l);
+  const unsigned w_blocks = loss_blocks((size_t)w.dst_rows * p.hblk * 4);
   // a workgroup's 64 rows are shared by as many as it takes to fill the chip
   const unsigned across = std::min<unsigned>((unsigned)p.hblk, std::max(1u, 1024u / (unsigned)(p.R / 64)));
-  auto rows_of_chunk = [&](int c, int grad) {
+  const LatticeRows z{r.at<bf16_t>(p.rows), r.x.plane, p.hblk, p.pa, (int)across};
+  const bool small = p.chunks == 1 && B <= 256 && (long long)B * U <= kLatticeSmall && p.R <= 16384;
+  if (small)
+    lattice_small_kernel<<<w_blocks + (unsigned)(p.R / 64) * across, 256, 0, s>>>(w, (int)w_blocks, l, r.chunk, z, r.at<unsigned>(p.ticket), p.R / 64);
+  else lattice_begin_kernel<<<1 + w_blocks, 256, 0, s>>>(w, l, r.at<unsigned>(p.ticket), p.R / 64);
+  auto rows_of_chunk = [&](int c) {
     r.chunk.c0 = c * p.R;
-    lattice_chunk_kernel<<<dim3((unsigned)(p.R / 64), across), 256, 0, s>>>(l, r.chunk, grad, r.at<bf16_t>(p.rows), r.x.plane, p.hblk, p.pa);
+    lattice_chunk_kernel<<<dim3((unsigned)(p.R / 64), across), 256, 0, s>>>(l, r.chunk, z);
   };
   for (int c = 0; c < p.chunks; ++c) {
-    rows_of_chunk(c, 0);
+    if (!small) rows_of_chunk(c);
     loss_stats(r, l.nodes);
   }
   const int both = p.grads, cells = U + 1;
@@ -550,7 +570,8 @@ int wind_transducer_loss(const wind_output_layer *layer, const void *e, int64_t 
     }
     const int columns = (p.hd + 255) / 256, n_e = fold.out[0] ? B * T * columns : 0, n_p = fold.out[1] ? B * (U + 1) * columns : 0;
     for (int c = 0; c < p.chunks; ++c) {
-      rows_of_chunk(c, 1);
+      if (!whole) rows_of_chunk(c);   // (a single chunk's are still there)
+      lattice_counts_kernel<<<p.R / 256, 256, 0, s>>>(l, r.chunk);
       const LossFinish f = loss_gradients(r, c, n_e + n_p > 0, LossOut{}, dw, db);
       const int blocks = f.n_db + f.n_dw + n_e + n_p;
       if (blocks) lattice_finish_kernel<<<(unsigned)blocks, 256, 0, s>>>(f, r.chunk, l, fold, n_e);

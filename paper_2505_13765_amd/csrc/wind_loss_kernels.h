@@ -23,6 +23,19 @@ namespace wind {
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr double kLn2 = 0.69314718055994530942;
 
+// Vectors at any address: the hardware takes them at every alignment (a row of 654 bf16 values begins at 4-byte steps; by single values W of 43250 such
+// rows was packed in 58 us).
+template <class V>
+__device__ __forceinline__ V load_any(const void *p) {
+  V v;
+  __builtin_memcpy(&v, p, sizeof(V));
+  return v;
+}
+template <class V>
+__device__ __forceinline__ void store_any(void *p, V v) {
+  __builtin_memcpy(p, &v, sizeof(V));
+}
+
 // ---- rows that count ----------------------------------------------------------------------------
 enum LossKind { kLossLabel = 0, kLossDistill = 1, kLossLattice = 2 };
 
@@ -52,7 +65,6 @@ __device__ __forceinline__ float group_sum(float v, int group) {
 __device__ __forceinline__ void loss_states(const LossRowsDev &r, int block, int nblocks, void *dh, int dtype, int H) {
   const int lane = threadIdx.x & 63, group = r.kind == kLossLabel ? 1 : loss_group(r.K), rows = 256 / group;
   const int l = threadIdx.x & (group - 1);
-  const bool wide = (uintptr_t)dh % 16 == 0 && (size_t)H * (dtype ? 2 : 4) % 16 == 0;
   for (long long n0 = (long long)block * rows; n0 < r.N; n0 += (long long)nblocks * rows) {
     const long long n = n0 + threadIdx.x / group;
     bool some = false, wrong = false;
@@ -78,18 +90,20 @@ __device__ __forceinline__ void loss_states(const LossRowsDev &r, int block, int
       out &= out - 1;
       const size_t bytes = (size_t)H * (dtype ? 2 : 4);
       char *row = (char *)dh + (size_t)(n0 + ((threadIdx.x & ~63) + at) / group) * bytes;
-      if (wide)
-        for (size_t c = lane * 16; c < bytes; c += 1024) *reinterpret_cast<u32x4 *>(row + c) = u32x4{0u, 0u, 0u, 0u};
-      else
-        for (size_t c = lane * 2; c < bytes; c += 128) *reinterpret_cast<uint16_t *>(row + c) = 0;
+      for (size_t c = lane * 16; c < bytes; c += 1024) {
+        if (c + 16 <= bytes) store_any(row + c, u32x4{0u, 0u, 0u, 0u});
+        else
+          for (size_t x = c; x < bytes; x += 2) *reinterpret_cast<uint16_t *>(row + x) = 0;
+      }
     }
   }
 }
 
 // One workgroup: the rows that count, in order.  A thread looks at 16 rows at a time.
-__global__ __launch_bounds__(1024) void loss_compact_kernel(LossRowsDev r) {
+__global__ __launch_bounds__(1024) void loss_compact_kernel(LossRowsDev r, unsigned *ticket, int tickets) {
   __shared__ int wave_sum_[16], total_;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  for (int i = tid; i < tickets; i += 1024) ticket[i] = 0u;
   if (tid == 0) total_ = 0;
   __syncthreads();
   for (long long base = 0; base < r.N; base += 16384) {
@@ -132,7 +146,6 @@ struct LossPack {
   bf16_t *dst;
   size_t plane;
   int dst_rows, blocks, planes;
-  int vec;                     // rows are 16-byte aligned
 };
 
 // 8 values as up to three planes
@@ -154,8 +167,8 @@ __device__ __forceinline__ void loss_split8(const float (&v)[8], int planes, bf1
 __device__ __forceinline__ void loss_load8(const LossPack &k, size_t row, int c, float (&v)[8]) {
   if (k.dtype) {
     const bf16_t *s = (const bf16_t *)k.src + row * k.stride + c;
-    if (k.vec && c + 8 <= k.cols) {
-      const u32x4 w = *reinterpret_cast<const u32x4 *>(s);
+    if (c + 8 <= k.cols) {
+      const u32x4 w = load_any<u32x4>(s);
 #pragma unroll
       for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
     } else {
@@ -164,8 +177,8 @@ __device__ __forceinline__ void loss_load8(const LossPack &k, size_t row, int c,
     }
   } else {
     const float *s = (const float *)k.src + row * k.stride + c;
-    if (k.vec && c + 8 <= k.cols) {
-      const f32x4 a = *reinterpret_cast<const f32x4 *>(s), b = *reinterpret_cast<const f32x4 *>(s + 4);
+    if (c + 8 <= k.cols) {
+      const f32x4 a = load_any<f32x4>(s), b = load_any<f32x4>(s + 4);
 #pragma unroll
       for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
     } else {
@@ -214,12 +227,12 @@ struct LossChunk {
 };
 __device__ __forceinline__ int chunk_rows(const LossChunk &k) { return min(max(*k.count - k.c0, 0), k.R); }
 
-// Entries of label and distillation rows.
-__device__ __forceinline__ void loss_entries(const LossRowsDev &r, const LossChunk &k, int block, int nblocks) {
-  const int live = chunk_rows(k), used = min((live + 255) & ~255, k.R);
+// Entries of label and distillation rows `begin` to `end` of a chunk, of which `live` count.
+__device__ __forceinline__ void loss_entries(const LossRowsDev &r, const LossChunk &k, int live, int begin, int end, int stride) {
   const int group = r.kind == kLossLabel ? 1 : loss_group(r.K), rows = 256 / group, l = threadIdx.x & (group - 1);
-  for (int i0 = block * rows; i0 < used; i0 += nblocks * rows) {
+  for (int i0 = begin; i0 < end; i0 += stride * rows) {
     const int i = i0 + (int)threadIdx.x / group;
+    if (i >= end) continue;
     if (i >= live) {
       for (int e = l; e < k.K; e += group) k.label[(size_t)e * k.R + i] = -1;
       if (l == 0) {
@@ -257,8 +270,95 @@ __device__ __forceinline__ void loss_entries(const LossRowsDev &r, const LossChu
 
 // The first launch of a chunk: its rows into panels, and their entries.
 __global__ __launch_bounds__(256) void loss_chunk_kernel(LossPack h, int pack_blocks, LossRowsDev r, LossChunk k) {
-  if ((int)blockIdx.x < pack_blocks) loss_pack(h, (int)blockIdx.x, pack_blocks);
-  else loss_entries(r, k, (int)blockIdx.x - pack_blocks, (int)gridDim.x - pack_blocks);
+  if ((int)blockIdx.x < pack_blocks) {
+    loss_pack(h, (int)blockIdx.x, pack_blocks);
+    return;
+  }
+  const int live = chunk_rows(k), block = (int)blockIdx.x - pack_blocks, group = r.kind == kLossLabel ? 1 : loss_group(r.K);
+  loss_entries(r, k, live, block * (256 / group), min((live + 255) & ~255, k.R), (int)gridDim.x - pack_blocks);
+}
+
+// Few rows, in one launch: W into panels, which rows count, and the rows' panels and entries.  Every workgroup of rows looks at all labels itself
+// (kLossSmall of them at most) and finds the places of its 64 rows among those that count; `across` of them share the 64 rows' panels.
+constexpr int kLossSmall = 16384, kLossSmallRows = 4096;
+__global__ __launch_bounds__(256) void loss_small_kernel(LossPack w, int w_blocks, LossRowsDev r, LossPack h, LossChunk k, int across, void *dh, unsigned *ticket,
+                                                         int tickets) {
+  __shared__ unsigned char state[kLossSmallRows];
+  __shared__ int sums[4];
+  if ((int)blockIdx.x < w_blocks) {
+    loss_pack(w, (int)blockIdx.x, w_blocks);
+    return;
+  }
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, block = (int)blockIdx.x - w_blocks, i0 = block / across * 64, part = block % across;
+  if (block == 0)
+    for (int i = tid; i < tickets; i += 256) ticket[i] = 0u;
+  // states of all rows; of the block's own source rows also what does not count
+  for (int n = tid; n < kLossSmallRows; n += 256) state[n] = 0;
+  __syncthreads();
+  const int group = r.kind == kLossLabel ? 1 : loss_group(r.K), rows = 256 / group, l = tid & (group - 1);
+  for (int n0 = 0; n0 < r.N; n0 += rows) {
+    const int n = n0 + tid / group;
+    bool some = false, wrong = false;
+    if (n < r.N)
+      for (int e = l; e < r.K; e += group) {
+        const int y = r.labels[(size_t)n * r.K + e];
+        wrong |= y >= r.V1;
+        some |= y >= 0 && (r.kind == kLossLabel || r.logits[(size_t)n * r.K + e] != -__builtin_inff());
+      }
+    for (int d = 1; d < group; d <<= 1) {
+      some |= __shfl_xor((int)some, d) != 0;
+      wrong |= __shfl_xor((int)wrong, d) != 0;
+    }
+    if (n >= r.N || l) continue;
+    state[n] = some && !wrong;
+    if (part == 0 && n >= i0 && n < i0 + 64 && !(some && !wrong)) r.loss[n] = wrong ? __builtin_nanf("") : 0.f;
+  }
+  __syncthreads();
+  // 16 rows a thread: their places
+  uint32_t bits = 0;
+  const u32x4 st = *reinterpret_cast<const u32x4 *>(state + tid * 16);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) bits |= ((st[i >> 2] >> (8 * (i & 3))) & 1u) << i;
+  const int mine = __popc(bits);
+  int sum = mine;
+  for (int d = 1; d < 64; d <<= 1) {
+    const int o = __shfl_up(sum, d);
+    if (lane >= d) sum += o;
+  }
+  if (lane == 63) sums[wave] = sum;
+  __syncthreads();
+  int put = sum - mine, live = 0;
+  for (int w2 = 0; w2 < 4; ++w2) {
+    if (w2 < wave) put += sums[w2];
+    live += sums[w2];
+  }
+  if (block == 0 && tid == 0) *r.count = live;
+  while (bits) {   // (the blocks of the same rows write the same)
+    if (put >= i0 && put < i0 + 64) r.idx[put] = tid * 16 + __builtin_ctz(bits);
+    ++put;
+    bits &= bits - 1;
+  }
+  __syncthreads();
+  const int used = min((live + 255) & ~255, k.R);
+  if (part == 0) loss_entries(r, k, live, i0, min(i0 + 64, used), 1);
+  if (i0 < used) {   // 64 rows, four threads each
+    const int row = i0 + (tid >> 2), q = tid & 3;
+    const size_t src = row < live ? (size_t)r.idx[row] : 0;
+    for (int blk = part; blk < h.blocks; blk += across) {
+      float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      const int c = blk * 32 + q * 8;
+      if (row < live && c < h.cols) loss_load8(h, src, c, v);
+      loss_split8(v, h.planes, h.dst + (size_t)blk * h.dst_rows * 32 + (size_t)row * 32 + q * 8, h.plane);
+    }
+  }
+  if (!dh) return;
+  for (int n = i0 + wave + 4 * part; n < min(i0 + 64, r.N); n += 4 * across) {   // gradients of rows that do not count
+    if (state[n]) continue;
+    for (int c = lane; c < h.cols; c += 64) {
+      if (h.dtype) ((bf16_t *)dh)[(size_t)n * h.cols + c] = 0;
+      else ((float *)dh)[(size_t)n * h.cols + c] = 0.f;
+    }
+  }
 }
 
 // ---- logits: statistics, and the gradient's logits ----------------------------------------------
@@ -308,19 +408,13 @@ struct LossEntries {
     for (int mi = 0; mi < T::MI; ++mi) hit |= __any(in[mi]) ? 1u << mi : 0u;
   }
   static __device__ __forceinline__ bool inside(int at) { return (unsigned)at < (unsigned)(32 * T::NI); }
-  // Entries of the lane's row of block mi, from e0 on: eight a lane, the row's two lanes one after the other.  at: column, or anything that is not
+  // More entries of row i, from e0 on: eight a lane, the row's two lanes one after the other.  at: column, or anything that is not
   // inside.  (All of a batch are asked for together: one by one, 64 entries a row cost as much again as the product of fp32 rows of 640.)
   static constexpr int kBatch = 16;
-  __device__ __forceinline__ void batch(const LossChunk &k, int mi, int i, int e0, int col0, int (&at)[8]) const {
+  __device__ __forceinline__ void batch(const LossChunk &k, int i, int e0, int col0, int (&at)[8]) const {
     const int half = (threadIdx.x & 63) >> 5;
 #pragma unroll
     for (int x = 0; x < 8; ++x) at[x] = -1;
-    if (k.K <= 2) {
-      at[0] = label[mi][0] - col0;
-      at[1] = label[mi][1] - col0;
-      if (half) at[0] = at[1] = -1;
-      return;
-    }
 #pragma unroll
     for (int x = 0; x < 8; ++x) {
       const int e = e0 + 8 * half + x;
@@ -343,8 +437,100 @@ __device__ __forceinline__ void loss_bias(const float *bias, int cols, int col0,
     }
 }
 
-template <class T>
-__global__ __launch_bounds__(256, T::W) void loss_stats_kernel(LossProduct g, LossChunk k, const float *bias) {
+// A probability as mantissa and exponent, m 2^e (wind_loss_lattice.h); zero has an exponent below every other's.
+struct Cell { float m; int e; };
+constexpr int kCellZero = -(1 << 28);
+__device__ __forceinline__ Cell cell_of_log2(float l) {   // 2^l, 1 <= m < 2
+  if (l == -__builtin_inff()) return Cell{0.f, kCellZero};
+  const float f = floorf(l);
+  return Cell{__builtin_amdgcn_exp2f(l - f), (int)f};
+}
+struct LossNodes {
+  float4 *arcs;                // per place of a lattice node: the probabilities of blank and of its label (m, e, m, e; e as bits)
+  int *slot;                   // [R] places of the chunk's nodes
+  float *lse2;                 // per node
+};
+// What the workgroups of a row tile leave for the one that joins it (JOIN) goes past their L2s, which do not see each other's.
+template <bool JOIN, class U>
+__device__ __forceinline__ void loss_leave(U *p, U v) {
+  if (JOIN) __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  else *p = v;
+}
+template <bool JOIN, class U>
+__device__ __forceinline__ U loss_take(const U *p) {
+  if (JOIN) return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return *p;
+}
+// Joins the column blocks of ROWS rows from i0 on, 256 / ROWS threads a row.  sm: 512 floats of LDS.
+template <int ROWS, bool JOIN>
+__device__ __forceinline__ void loss_rows_done(const LossRowsDev &r, const LossChunk &k, int live, int parts, const LossNodes &nodes, int i0, float *sm) {
+  constexpr int G = 256 / ROWS;
+  float *const ss = sm + 256;
+  const int lane = threadIdx.x % ROWS, grp = threadIdx.x / ROWS, i = i0 + lane;
+  float m = -__builtin_inff(), s = 0.f;
+  if (i < live) {
+#pragma unroll 4
+    for (int p = grp; p < parts; p += G) {
+      const float2 v = __builtin_bit_cast(float2, loss_take<JOIN>(reinterpret_cast<const unsigned long long *>(k.part) + (size_t)p * k.R + i));
+      const float top = fmaxf(m, v.x), ref = top == -__builtin_inff() ? 0.f : top;
+      s = s * __builtin_amdgcn_exp2f(m - ref) + v.y * __builtin_amdgcn_exp2f(v.x - ref);
+      m = top;
+    }
+  }
+  sm[threadIdx.x] = m;
+  ss[threadIdx.x] = s;
+  __syncthreads();
+  float top = sm[lane];
+#pragma unroll 16
+  for (int q = 1; q < G; ++q) top = fmaxf(top, sm[q * ROWS + lane]);
+  const float ref = top == -__builtin_inff() ? 0.f : top;
+  s = 0.f;
+#pragma unroll 16
+  for (int q = 0; q < G; ++q) s += ss[q * ROWS + lane] * __builtin_amdgcn_exp2f(sm[q * ROWS + lane] - ref);
+  const float ls = log2f(s);
+  // -log2 p of entry e
+  auto cost = [&](int e) { return __builtin_fmaf(-loss_take<JOIN>(k.logit + (size_t)e * k.R + i), k.c, top) + ls; };
+  const bool first = grp == 0 && i < live;
+  if (first) k.lse2[i] = top + ls;
+  float sum = 0.f;
+  if (r.kind == kLossLattice) {
+    if (first) {
+      const Cell stay = cell_of_log2(-cost(0)), take = cell_of_log2(k.label[(size_t)k.R + i] < 0 ? -__builtin_inff() : -cost(1));
+      nodes.lse2[k.c0 + i] = top + ls;
+      nodes.arcs[nodes.slot[i]] = make_float4(stay.m, __int_as_float(stay.e), take.m, __int_as_float(take.e));
+    }
+  } else if (r.kind == kLossLabel) {
+    if (first) r.loss[r.idx[k.c0 + i]] = cost(0) * (float)kLn2;
+  } else {
+    if (i < live) {
+#pragma unroll 4
+      for (int e = grp; e < k.K; e += G) {
+        const float lq = k.value[(size_t)e * k.R + i], q = exp2f(lq);   // (an entry that is not there has q = 0)
+        if (q != 0.f) sum += q * (lq + cost(e));
+      }
+    }
+    __syncthreads();
+    sm[threadIdx.x] = sum;
+    __syncthreads();
+    if (first) {
+#pragma unroll 16
+      for (int q = 1; q < G; ++q) sum += sm[q * ROWS + lane];
+      r.loss[r.idx[k.c0 + i]] = sum * (float)kLn2 * r.tau * r.tau;
+    }
+  }
+  __syncthreads();
+}
+template <int ROWS>
+__global__ __launch_bounds__(256) void loss_rows_done_kernel(LossRowsDev r, LossChunk k, int parts, LossNodes nodes) {
+  __shared__ float sm[512];
+  const int live = chunk_rows(k);
+  if ((int)blockIdx.x * ROWS < live) loss_rows_done<ROWS, false>(r, k, live, parts, nodes, (int)blockIdx.x * ROWS, sm);
+}
+
+// Row statistics.  JOIN: the last workgroup of a row tile (by a ticket, zero at launch) joins its column blocks itself; few rows and column blocks,
+// where a launch of its own costs more.
+template <class T, bool JOIN>
+__global__ __launch_bounds__(256, T::W) void loss_stats_kernel(LossProduct g, LossChunk k, const float *bias, LossRowsDev r, LossNodes nodes, unsigned *ticket) {
   __shared__ __attribute__((aligned(256))) unsigned char smem[T::SMEM];
   const int live = chunk_rows(k);
   int ti, tj, split;
@@ -375,90 +561,36 @@ __global__ __launch_bounds__(256, T::W) void loss_stats_kernel(LossProduct g, Lo
 #pragma unroll
       for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[mi][ni][r], k.c, -ref));
     sum += xor32_f32(sum);
-    if (lane < 32 && col0 < g.cols) k.part[(size_t)(col0 / (32 * T::NI)) * k.R + i] = make_float2(mc, sum);
+    if (lane < 32 && col0 < g.cols)
+      loss_leave<JOIN>(reinterpret_cast<unsigned long long *>(k.part) + (size_t)(col0 / (32 * T::NI)) * k.R + i,
+                       __builtin_bit_cast(unsigned long long, make_float2(mc, sum)));
     if (entries.hit >> mi & 1u) {
       loss_tile_out<T>(acc[mi], tile);
-      for (int e0 = 0; e0 < k.K; e0 += entries.kBatch) {
+      if (k.K <= 2) {   // a lane each
+        const int at = (lane < 32 ? entries.label[mi][0] : entries.label[mi][1]) - col0;
+        if (entries.inside(at)) loss_leave<JOIN>(k.logit + (size_t)(lane >> 5) * k.R + i, tile[(lane & 31) * T::PITCH + at]);
+      } else for (int e0 = 0; e0 < k.K; e0 += entries.kBatch) {
         int at[8];
-        entries.batch(k, mi, i, e0, col0, at);
+        entries.batch(k, i, e0, col0, at);
 #pragma unroll
         for (int x = 0; x < 8; ++x)
-          if (entries.inside(at[x])) k.logit[(size_t)(e0 + 8 * (lane >> 5) + x) * k.R + i] = tile[(lane & 31) * T::PITCH + at[x]];
+          if (entries.inside(at[x])) loss_leave<JOIN>(k.logit + (size_t)(e0 + 8 * (lane >> 5) + x) * k.R + i, tile[(lane & 31) * T::PITCH + at[x]]);
       }
       __builtin_amdgcn_wave_barrier();
     }
   }
-}
-
-// Joins a row's column blocks: 16 rows a workgroup, 16 threads a row.
-// A probability as mantissa and exponent, m 2^e (wind_loss_lattice.h); zero has an exponent below every other's.
-struct Cell { float m; int e; };
-constexpr int kCellZero = -(1 << 28);
-__device__ __forceinline__ Cell cell_of_log2(float l) {   // 2^l, 1 <= m < 2
-  if (l == -__builtin_inff()) return Cell{0.f, kCellZero};
-  const float f = floorf(l);
-  return Cell{__builtin_amdgcn_exp2f(l - f), (int)f};
-}
-struct LossNodes {
-  float4 *arcs;                // per place of a lattice node: the probabilities of blank and of its label (m, e, m, e; e as bits)
-  int *slot;                   // [R] places of the chunk's nodes
-  float *lse2;                 // per node
-};
-__global__ __launch_bounds__(256) void loss_rows_done_kernel(LossRowsDev r, LossChunk k, int parts, LossNodes nodes) {
-  __shared__ float sm[16][16], ss[16][16];
-  const int live = chunk_rows(k), lane = threadIdx.x & 15, grp = threadIdx.x >> 4;
-  if ((int)blockIdx.x * 16 >= live) return;
-  const int i = blockIdx.x * 16 + lane;
-  float m = -__builtin_inff(), s = 0.f;
-  if (i < live) {
-#pragma unroll 4
-    for (int p = grp; p < parts; p += 16) {
-      const float2 v = k.part[(size_t)p * k.R + i];
-      const float top = fmaxf(m, v.x), ref = top == -__builtin_inff() ? 0.f : top;
-      s = s * __builtin_amdgcn_exp2f(m - ref) + v.y * __builtin_amdgcn_exp2f(v.x - ref);
-      m = top;
-    }
-  }
-  sm[grp][lane] = m;
-  ss[grp][lane] = s;
+  if (!JOIN) return;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // what this wave leaves has arrived
+  int &last = *reinterpret_cast<int *>(smem + 4096);
   __syncthreads();
-  float top = sm[0][lane];
-#pragma unroll
-  for (int q = 1; q < 16; ++q) top = fmaxf(top, sm[q][lane]);
-  const float ref = top == -__builtin_inff() ? 0.f : top;
-  s = 0.f;
-#pragma unroll
-  for (int q = 0; q < 16; ++q) s += ss[q][lane] * __builtin_amdgcn_exp2f(sm[q][lane] - ref);
-  const float ls = log2f(s);
-  // -log2 p of entry e
-  auto cost = [&](int e) { return __builtin_fmaf(-k.logit[(size_t)e * k.R + i], k.c, top) + ls; };
-  if (grp == 0 && i < live) k.lse2[i] = top + ls;
-  if (r.kind == kLossLattice) {
-    if (grp || i >= live) return;
-    const Cell stay = cell_of_log2(-cost(0)), take = cell_of_log2(k.label[(size_t)k.R + i] < 0 ? -__builtin_inff() : -cost(1));
-    nodes.lse2[k.c0 + i] = top + ls;
-    nodes.arcs[nodes.slot[i]] = make_float4(stay.m, __int_as_float(stay.e), take.m, __int_as_float(take.e));
-    return;
-  }
-  if (r.kind == kLossLabel) {
-    if (grp == 0 && i < live) r.loss[r.idx[k.c0 + i]] = cost(0) * (float)kLn2;
-    return;
-  }
-  float sum = 0.f;
-  if (i < live) {
-#pragma unroll 4
-    for (int e = grp; e < k.K; e += 16) {
-      const float lq = k.value[(size_t)e * k.R + i], q = exp2f(lq);   // (an entry that is not there has q = 0)
-      if (q != 0.f) sum += q * (lq + cost(e));
-    }
-  }
+  if (threadIdx.x == 0) last = __hip_atomic_fetch_add(ticket + ti, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)g.ct - 1u;
   __syncthreads();
-  sm[grp][lane] = sum;
-  __syncthreads();
-  if (grp || i >= live) return;
-#pragma unroll
-  for (int q = 1; q < 16; ++q) sum += sm[q][lane];
-  r.loss[r.idx[k.c0 + i]] = sum * (float)kLn2 * r.tau * r.tau;
+  if (!last) return;
+  const int end = min(live, (ti + 1) * T::BM), parts = (g.cols + 32 * T::NI - 1) / (32 * T::NI);
+  float *const sm = reinterpret_cast<float *>(smem);
+  if (end - ti * T::BM <= 16) loss_rows_done<16, true>(r, k, end, parts, nodes, ti * T::BM, sm);
+  else
+    for (int i = ti * T::BM; i < end; i += 64) loss_rows_done<64, true>(r, k, end, parts, nodes, i, sm);
 }
 
 // dx of a chunk, in panels, and its column sums.
@@ -496,10 +628,18 @@ __global__ __launch_bounds__(256, T::W) void loss_dx_kernel(LossProduct g, LossC
     if (entries.hit >> mi & 1u) {
       loss_tile_out<T>(acc[mi], tile);
       float *row = tile + (lane & 31) * T::PITCH;
-      for (int e0 = 0; e0 < k.K; e0 += entries.kBatch) {
+      if (k.K <= 2) {
+        const int at[2] = {entries.label[mi][0] - col0, entries.label[mi][1] - col0};
+        const float c[2] = {k.coef[i], k.K > 1 ? k.coef[k.R + i] : 0.f};
+        if (half == 0) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            if (entries.inside(at[e])) row[at[e]] -= c[e];
+        }
+      } else for (int e0 = 0; e0 < k.K; e0 += entries.kBatch) {
         int at[8];
         float c[8];
-        entries.batch(k, mi, i, e0, col0, at);
+        entries.batch(k, i, e0, col0, at);
 #pragma unroll
         for (int x = 0; x < 8; ++x) c[x] = e0 + 8 * half + x < k.K ? k.coef[(size_t)(e0 + 8 * half + x) * k.R + i] : 0.f;
 #pragma unroll
@@ -579,44 +719,60 @@ struct LossOut {
   size_t ld;                   // values between rows
   int dtype;                   // 0: fp32, 1: bf16
   int cols;
-  int vec;                     // four values of a row can be stored at once
   const int *idx;              // null, or row i goes to row idx[i]
   int add;                     // fp32: added to what is there
   int splits;                  // > 1: fp32, the s-th part of the sum goes to p + s part
   size_t part;
 };
+// 32 rows of results from LDS, RUN values of a row per lane
+template <int RUN>
+__device__ __forceinline__ void loss_store_rows(const LossOut &o, const float *tile, int pitch, int width, int i0, int rows, int j0, size_t base) {
+  const int lane = threadIdx.x & 63, per = width / RUN;
+  for (int u = lane; u < 32 * per; u += 64) {
+    const int r = u / per, c = (u - r * per) * RUN, i = i0 + r, j = j0 + c;
+    if (i >= rows || j >= o.cols) continue;
+    const size_t at = base + (size_t)(o.idx ? o.idx[i] : i) * o.ld + j;
+    float v[RUN];
+#pragma unroll
+    for (int e = 0; e < RUN; ++e) v[e] = tile[r * pitch + c + e];
+    const bool whole = j + RUN <= o.cols;
+    if constexpr (RUN == 8) {
+      bf16_t *d = (bf16_t *)o.p + at;
+      if (whole) store_any(d, u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])});
+      else
+#pragma unroll
+        for (int e = 0; e < RUN; ++e)
+          if (j + e < o.cols) d[e] = (bf16_t)f32_to_bf16_bits(v[e]);
+    } else {
+      float *d = (float *)o.p + at;
+      if (whole) {
+        const f32x4 x = {v[0], v[1], v[2], v[3]};
+        store_any(d, o.add ? load_any<f32x4>(d) + x : x);
+      } else
+#pragma unroll
+        for (int e = 0; e < RUN; ++e)
+          if (j + e < o.cols) d[e] = o.add ? d[e] + v[e] : v[e];
+    }
+  }
+}
+// A wave's results, 32 rows at a time through LDS: what a store instruction writes is then whole lines of a few rows, not a piece of 32 of them
+// (dW of 43250 x 654 for 9 rows: 89 us by pieces).
 template <class T>
-__device__ __forceinline__ void loss_store(const LossOut &o, const f32x16 (&acc)[T::MI][T::NI], int i0, int rows, int j0, int split) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), half = lane >> 5;
+__device__ __forceinline__ void loss_store(const LossOut &o, const f32x16 (&acc)[T::MI][T::NI], int i0, int rows, int j0, int split, unsigned char *smem) {
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  float *tile = reinterpret_cast<float *>(smem) + wave * 32 * T::PITCH;
+  const int j = j0 + (wave & 1) * 32 * T::NI;
+  if (j >= o.cols) return;
 #pragma unroll
   for (int mi = 0; mi < T::MI; ++mi) {
-    const int i = i0 + ((wave >> 1) * T::MI + mi) * 32 + (lane & 31);
-    if (i >= rows) continue;
-    const size_t at = (size_t)(o.idx ? o.idx[i] : i) * o.ld + (size_t)split * o.part;
-#pragma unroll
-    for (int ni = 0; ni < T::NI; ++ni)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int j = j0 + ((wave & 1) * T::NI + ni) * 32 + 8 * q + 4 * half;
-        if (j >= o.cols) continue;
-        f32x4 v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = acc[mi][ni][4 * q + e];
-        if (o.dtype) {
-          bf16_t *d = (bf16_t *)o.p + at + j;
-          if (o.vec && j + 4 <= o.cols) *reinterpret_cast<u32x2 *>(d) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-          else
-            for (int e = 0; e < 4 && j + e < o.cols; ++e) d[e] = (bf16_t)f32_to_bf16_bits(v[e]);
-        } else {
-          float *d = (float *)o.p + at + j;
-          if (o.vec && j + 4 <= o.cols) {
-            f32x4 *w = reinterpret_cast<f32x4 *>(d);
-            *w = o.add ? *w + v : v;
-          } else {
-            for (int e = 0; e < 4 && j + e < o.cols; ++e) d[e] = o.add ? d[e] + v[e] : v[e];
-          }
-        }
-      }
+    const int i = i0 + ((wave >> 1) * T::MI + mi) * 32;
+    if (i >= rows) break;
+    loss_tile_out<T>(acc[mi], tile);
+    const size_t base = (size_t)split * o.part;
+    if (o.dtype) loss_store_rows<8>(o, tile, T::PITCH, 32 * T::NI, i, rows, j, base);
+    else loss_store_rows<4>(o, tile, T::PITCH, 32 * T::NI, i, rows, j, base);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
@@ -637,7 +793,7 @@ __device__ __forceinline__ void loss_product(int bid, const LossProduct &g, cons
   f32x16 acc[T::MI][T::NI];
   if (s0 < s1) loss_mainloop<T, TA, TB>(g.a, g.b, ti * T::BM, tj * T::BN, s0, s1, smem, acc, [&]() { loss_clear<T>(acc); });
   else loss_clear<T>(acc);
-  loss_store<T>(o, acc, ti * T::BM, rows, tj * T::BN, split);
+  loss_store<T>(o, acc, ti * T::BM, rows, tj * T::BN, split, smem);
 }
 // dz = dx W: rows of the chunk against columns of W's panels, summed over outputs.
 template <class T>
@@ -652,6 +808,15 @@ __global__ __launch_bounds__(256, T::W) void loss_dw_kernel(LossProduct g, LossC
   const int live = chunk_rows(k);
   if (o.add && live == 0) return;
   loss_product<T, true, true>((int)blockIdx.x, g, o, g.cols, (live + 31) / 32, smem);
+}
+
+// Both in one launch, on tiles of one shape.
+template <class T>
+__global__ __launch_bounds__(256, T::W) void loss_products_kernel(LossProduct z, LossOut zo, int z_blocks, LossProduct w, LossOut wo, LossChunk k) {
+  __shared__ __attribute__((aligned(256))) unsigned char smem[T::SMEM];
+  const int live = chunk_rows(k);
+  if ((int)blockIdx.x < z_blocks) loss_product<T, false, true>((int)blockIdx.x, z, zo, live, z.slabs, smem);
+  else if (!wo.add || live) loss_product<T, true, true>((int)blockIdx.x - z_blocks, w, wo, w.cols, (live + 31) / 32, smem);
 }
 
 // ---- the last launch of a chunk -----------------------------------------------------------------
@@ -684,7 +849,7 @@ struct LossJoin {
   const float *parts;
   int splits;
   size_t part, ld;
-  int rows, cols, dtype, vec;
+  int rows, cols, dtype;
   const int *idx;
   void *out;                   // [.., cols]
 };
@@ -697,9 +862,9 @@ __device__ __forceinline__ void loss_join(const LossJoin &j, int rows, int block
     f32x4 s = *reinterpret_cast<const f32x4 *>(j.parts + v * j.ld + h);
     for (int q = 1; q < j.splits; ++q) s += *reinterpret_cast<const f32x4 *>(j.parts + (size_t)q * j.part + v * j.ld + h);
     const size_t to = (j.idx ? (size_t)j.idx[v] : v) * j.cols + h;
-    if (j.vec) {
-      if (j.dtype) *reinterpret_cast<u32x2 *>((bf16_t *)j.out + to) = u32x2{pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3])};
-      else *reinterpret_cast<f32x4 *>((float *)j.out + to) = s;
+    if (h + 4 <= j.cols) {
+      if (j.dtype) store_any((bf16_t *)j.out + to, u32x2{pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3])});
+      else store_any((float *)j.out + to, s);
       continue;
     }
     for (int e = 0; e < 4 && h + e < j.cols; ++e) {

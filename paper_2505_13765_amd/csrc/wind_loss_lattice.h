@@ -20,7 +20,6 @@ struct LatticeDev {
   int B, T, U, V1, H, dtype;
   const void *e, *p;                          // e [B, T, H], p [B, U + 1, H]
   long long e_b, e_t, p_b, p_u;               // strides in values
-  int vec;                                    // their rows are 16-byte aligned
   const int *labels, *frames, *counts;        // [B, U], [B], [B]
   const float *weights;                       // [B] or null
   float *loss;                                // [B]
@@ -35,24 +34,36 @@ __device__ __forceinline__ int lattice_place(const LatticeDev &l, int first, int
 __device__ __forceinline__ const char *lattice_e(const LatticeDev &l, int b, int t) { return (const char *)l.e + (b * l.e_b + t * l.e_t) * (l.dtype ? 2 : 4); }
 __device__ __forceinline__ const char *lattice_p(const LatticeDev &l, int b, int u) { return (const char *)l.p + (b * l.p_b + u * l.p_u) * (l.dtype ? 2 : 4); }
 
-// One workgroup: which utterances count, and where their rows begin.
-__device__ __forceinline__ void lattice_rows(const LatticeDev &l) {
+// One workgroup: which utterances count, and where their rows begin; returns the number of rows.
+__device__ __forceinline__ int lattice_rows(const LatticeDev &l) {
   __shared__ int wave_sum_[2][4], total_[2];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  for (int b = wave; b < l.B; b += 4) {
-    const int T = min(max(l.frames[b], 0), l.T), U = min(max(l.counts[b], 0), l.U);
+  // the lanes of a group look through an utterance's labels
+  int group = 1;
+  while (group < 64 && group < l.U) group <<= 1;
+  const int at_once = 256 / group, g = tid / group, x = tid & (group - 1);
+  for (int b0 = 0; b0 < l.B; b0 += at_once) {
+    const int b = b0 + g;
+    int T = 0, U = 0;
     bool bad = false;
-    for (int u = lane; u < U; u += 64) {
-      const int y = l.labels[(size_t)b * l.U + u];
-      bad |= y < 0 || y >= l.V1 - 1;
+    if (b < l.B) {
+      T = min(max(l.frames[b], 0), l.T);
+      U = min(max(l.counts[b], 0), l.U);
+#pragma unroll 2
+      for (int u = x; u < U; u += group) {
+        const int y = l.labels[(size_t)b * l.U + u];
+        bad |= y < 0 || y >= l.V1 - 1;
+      }
     }
-    const bool wrong = __any(bad) && T > 0;
-    if (lane == 0) {
+    for (int d = 1; d < group; d <<= 1) bad |= __shfl_xor((int)bad, d) != 0;
+    if (b < l.B && x == 0) {
+      const bool wrong = bad && T > 0;
       l.tb[b] = wrong ? 0 : T;
       l.ub[b] = U;
       if (wrong || T == 0) l.loss[b] = wrong ? __builtin_nanf("") : 0.f;
     }
   }
+  __syncthreads();
   if (tid < 2) total_[tid] = 0;
   __syncthreads();
   for (int base = 0; base < l.B; base += 256) {
@@ -89,10 +100,15 @@ __device__ __forceinline__ void lattice_rows(const LatticeDev &l) {
     l.off[l.B] = total_[0];
     *l.count = total_[0];
   }
+  __syncthreads();
+  return total_[0];
 }
 // The first launch of a call: the rows, and W into panels.
-__global__ __launch_bounds__(256) void lattice_begin_kernel(LossPack w, LatticeDev l) {
-  if (blockIdx.x == 0) lattice_rows(l);
+__global__ __launch_bounds__(256) void lattice_begin_kernel(LossPack w, LatticeDev l, unsigned *ticket, int tickets) {
+  if (blockIdx.x == 0) {
+    for (int i = threadIdx.x; i < tickets; i += 256) ticket[i] = 0u;
+    lattice_rows(l);
+  }
   else loss_pack(w, (int)blockIdx.x - 1, (int)gridDim.x - 1);
 }
 
@@ -199,38 +215,51 @@ __global__ __launch_bounds__(MULTI ? 1024 : 64) void lattice_sums_kernel(Lattice
   else lattice_run<C, AHEAD, MULTI, false>(l, b, both, edge);
 }
 
-// The first launch of a chunk: its rows z = relu(e + p) in panels, their two entries (0: blank, 1: the next label), and for the gradient
-// the arcs' expected counts.  A workgroup takes 64 rows, four threads a row.
-__global__ __launch_bounds__(256) void lattice_chunk_kernel(LatticeDev l, LossChunk k, int grad, bf16_t *dst, size_t plane, int blocks, int planes) {
-  const int live = chunk_rows(k), used = min((live + 255) & ~255, k.R);
-  const int i = blockIdx.x * 64 + (threadIdx.x >> 2), q = threadIdx.x & 3;
-  if (i >= used) return;
-  bf16_t *to = dst + (size_t)i * 32 + q * 8;
-  if (i >= live) {
-    const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int blk = blockIdx.y; blk < blocks; blk += gridDim.y) loss_split8(none, planes, to + (size_t)blk * k.R * 32, plane);
-    if (q == 0 && blockIdx.y == 0) {
-      k.label[i] = k.label[k.R + i] = -1;
-      k.scale[i] = 0.f;
-      k.lse2[i] = __builtin_inff();
-    }
-    return;
-  }
-  const int n = k.c0 + i;
+// A chunk's rows, 64 from i0 on and four threads each: z = relu(e + p) in panels (of the panels, every `across`-th from `part` on), and their two
+// entries (0: blank, 1: the next label).
+struct LatticeRows {
+  bf16_t *dst;
+  size_t plane;
+  int blocks, planes, across;
+};
+struct LatticeNode { int b, t, u, U1, place; };
+__device__ __forceinline__ LatticeNode lattice_node(const LatticeDev &l, int n) {
   int lo = 0, hi = l.B;          // the last utterance whose first row is at or before n: it has rows
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     if (l.off[mid] <= n) lo = mid;
     else hi = mid;
   }
-  const int b = lo, U1 = l.ub[b] + 1, at = n - l.off[b], t = at / U1, u = at - t * U1;
+  LatticeNode d;
+  d.b = lo;
+  d.U1 = l.ub[lo] + 1;
+  const int at = n - l.off[lo];
+  d.t = at / d.U1;
+  d.u = at - d.t * d.U1;
+  d.place = lattice_place(l, l.place[lo], d.U1, d.u) + d.t * d.U1;
+  return d;
+}
+__device__ __forceinline__ void lattice_chunk(const LatticeDev &l, const LossChunk &k, const LatticeRows &z, int live, int i0, int part) {
+  const int used = min((live + 255) & ~255, k.R), i = i0 + (threadIdx.x >> 2), q = threadIdx.x & 3;
+  if (i >= used) return;
+  bf16_t *to = z.dst + (size_t)i * 32 + q * 8;
+  if (i >= live) {
+    const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int blk = part; blk < z.blocks; blk += z.across) loss_split8(none, z.planes, to + (size_t)blk * k.R * 32, z.plane);
+    if (q == 0 && part == 0) {
+      k.label[i] = k.label[k.R + i] = -1;
+      k.scale[i] = 0.f;
+      k.lse2[i] = __builtin_inff();
+    }
+    return;
+  }
+  const LatticeNode d = lattice_node(l, k.c0 + i);
   LossPack e{}, p{};
   e.dtype = p.dtype = l.dtype;
   e.cols = p.cols = l.H;
-  e.vec = p.vec = l.vec;
-  e.src = lattice_e(l, b, t);
-  p.src = lattice_p(l, b, u);
-  for (int blk = blockIdx.y; blk < blocks; blk += gridDim.y) {
+  e.src = lattice_e(l, d.b, d.t);
+  p.src = lattice_p(l, d.b, d.u);
+  for (int blk = part; blk < z.blocks; blk += z.across) {
     const int c = blk * 32 + q * 8;
     float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (c < l.H) {
@@ -240,23 +269,45 @@ __global__ __launch_bounds__(256) void lattice_chunk_kernel(LatticeDev l, LossCh
 #pragma unroll
       for (int j = 0; j < 8; ++j) { x[j] += y[j]; x[j] = x[j] > 0.f || x[j] != x[j] ? x[j] : 0.f; }   // NaN stays
     }
-    loss_split8(x, planes, to + (size_t)blk * k.R * 32, plane);
+    loss_split8(x, z.planes, to + (size_t)blk * k.R * 32, z.plane);
   }
-  if (q || blockIdx.y) return;
-  const int place = lattice_place(l, l.place[b], U1, u) + t * U1;
-  l.nodes.slot[i] = place;
+  if (q || part) return;
+  l.nodes.slot[i] = d.place;
   k.label[i] = l.V1 - 1;
-  k.label[k.R + i] = u + 1 < U1 ? l.labels[(size_t)b * l.U + u] : -1;
-  if (!grad) return;
-  const Cell P = cell_unpack(l.beta[l.place[b]]), a = cell_unpack(l.alpha[place]);
-  const float4 arcs = l.nodes.arcs[place];
-  const float w = l.weights ? l.weights[b] : 1.f;
-  auto share = [&](float m, float e_bits, Cell next) {   // expected count of an arc, times the utterance's weight
+  k.label[k.R + i] = d.u + 1 < d.U1 ? l.labels[(size_t)d.b * l.U + d.u] : -1;
+}
+__global__ __launch_bounds__(256) void lattice_chunk_kernel(LatticeDev l, LossChunk k, LatticeRows z) {
+  lattice_chunk(l, k, z, chunk_rows(k), (int)blockIdx.x * 64, (int)blockIdx.y);
+}
+// Few utterances with few labels, in one launch: W into panels, and the rows, which every workgroup counts for itself.
+constexpr int kLatticeSmall = 1024;   // B * U
+__global__ __launch_bounds__(256) void lattice_small_kernel(LossPack w, int w_blocks, LatticeDev l, LossChunk k, LatticeRows z, unsigned *ticket, int tickets) {
+  if ((int)blockIdx.x < w_blocks) {
+    loss_pack(w, (int)blockIdx.x, w_blocks);
+    return;
+  }
+  const int block = (int)blockIdx.x - w_blocks;
+  if (block == 0)
+    for (int i = threadIdx.x; i < tickets; i += 256) ticket[i] = 0u;
+  const int rows = lattice_rows(l);
+  lattice_chunk(l, k, z, min(rows, k.R), block / z.across * 64, block % z.across);
+}
+
+// The gradient's scales and coefficients of a chunk's rows: the arcs' expected counts, times the utterance's weight.
+__global__ __launch_bounds__(256) void lattice_counts_kernel(LatticeDev l, LossChunk k) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= chunk_rows(k)) return;
+  const int n = k.c0 + i;
+  const LatticeNode d = lattice_node(l, n);
+  const Cell P = cell_unpack(l.beta[l.place[d.b]]), a = cell_unpack(l.alpha[d.place]);
+  const float4 arcs = l.nodes.arcs[d.place];
+  const float w = l.weights ? l.weights[d.b] : 1.f;
+  auto share = [&](float m, float e_bits, Cell next) {
     return P.m == 0.f ? 0.f : w * __builtin_amdgcn_ldexpf(a.m * m * next.m / P.m, a.e + __float_as_int(e_bits) + next.e - P.e);
   };
-  const bool last = t + 1 == l.tb[b], more = u + 1 < U1;
-  const float by_blank = last ? (more ? 0.f : share(arcs.x, arcs.y, Cell{0.5f, 1})) : share(arcs.x, arcs.y, cell_unpack(l.beta[place + U1]));
-  const float by_label = more ? share(arcs.z, arcs.w, cell_unpack(l.beta[lattice_place(l, l.place[b], U1, u + 1) + t * U1])) : 0.f;
+  const bool last = d.t + 1 == l.tb[d.b], more = d.u + 1 < d.U1;
+  const float by_blank = last ? (more ? 0.f : share(arcs.x, arcs.y, Cell{0.5f, 1})) : share(arcs.x, arcs.y, cell_unpack(l.beta[d.place + d.U1]));
+  const float by_label = more ? share(arcs.z, arcs.w, cell_unpack(l.beta[lattice_place(l, l.place[d.b], d.U1, d.u + 1) + d.t * d.U1])) : 0.f;
   k.coef[i] = by_blank;
   k.coef[k.R + i] = by_label;
   k.scale[i] = by_blank + by_label;
@@ -277,20 +328,25 @@ __device__ __forceinline__ f32x4 lattice_load4(const LatticeDev &l, const char *
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
   if (l.dtype) {
     const bf16_t *s = (const bf16_t *)row + c;
-    if (l.vec && c + 4 <= l.H) {
-      const u32x2 w = *reinterpret_cast<const u32x2 *>(s);
+    if (c + 4 <= l.H) {
+      const u32x2 w = load_any<u32x2>(s);
       v = f32x4{__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xFFFF0000u), __uint_as_float(w[1] << 16), __uint_as_float(w[1] & 0xFFFF0000u)};
     } else
       for (int j = 0; j < 4; ++j) v[j] = c + j < l.H ? bf16_bits_to_f32(s[j]) : 0.f;
   } else {
     const float *s = (const float *)row + c;
-    if (l.vec && c + 4 <= l.H) v = *reinterpret_cast<const f32x4 *>(s);
+    if (c + 4 <= l.H) v = load_any<f32x4>(s);
     else
       for (int j = 0; j < 4; ++j) v[j] = c + j < l.H ? s[j] : 0.f;
   }
   return v;
 }
 __device__ __forceinline__ void lattice_store4(const LatticeDev &l, void *out, size_t row, int c, f32x4 v) {
+  if (c + 4 <= l.H) {
+    if (l.dtype) store_any((bf16_t *)out + row * l.H + c, u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])});
+    else store_any((float *)out + row * l.H + c, v);
+    return;
+  }
   for (int j = 0; j < 4 && c + j < l.H; ++j) {
     if (l.dtype) ((bf16_t *)out)[row * l.H + c + j] = (bf16_t)f32_to_bf16_bits(v[j]);
     else ((float *)out)[row * l.H + c + j] = v[j];

@@ -10,6 +10,7 @@ those gradients in the order asked for: the gradients of sum(weights * losses), 
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 from typing import Optional, Sequence
 
@@ -20,17 +21,18 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _take(t, name, shape, dtype, like=None, dense=True):
+def _take(t, name, shape, dtype, device, dense=True):
     """Checks one argument; None passes."""
     if t is None:
         return
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+    if t.dtype is not dtype or t.shape != shape:
         raise ValueError(f"{name} must be {str(dtype)[6:]} of shape {tuple(shape)}, got {str(t.dtype)[6:]} of shape {tuple(t.shape)}")
-    if not t.is_cuda or (like is not None and t.device != like.device):
+    if not t.is_cuda or t.device != device:
         raise ValueError(f"{name} must be on the GPU of the other arguments")
-    if dense and not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    if not dense and (t.stride(-1) != 1 and t.shape[-1] > 1 or any(s < 0 for s in t.stride())):
+    if dense:
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+    elif t.shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError(f"{name}'s last axis must be contiguous")
 
 
@@ -40,12 +42,21 @@ def _layer(w_out, b_out):
     if w_out.dim() != 2 or w_out.dtype not in (torch.float32, torch.bfloat16):
         raise ValueError("w_out must be a float32 or bfloat16 matrix")
     V1, H = w_out.shape
-    _take(w_out, "w_out", (V1, H), w_out.dtype, dense=False)
-    _take(b_out, "b_out", (V1,), torch.float32, w_out)
-    if V1 > 1 and w_out.stride(0) < H:
+    device = w_out.device
+    _take(w_out, "w_out", (V1, H), w_out.dtype, device, dense=False)
+    _take(b_out, "b_out", (V1,), torch.float32, device)
+    stride = w_out.stride(0) if V1 > 1 else H
+    if stride < H:
         raise ValueError("w_out's rows must not overlap")
-    return OutputLayer(_ptr(w_out), _ptr(b_out), max(int(w_out.stride(0)), H), V1, H,
+    return OutputLayer(_ptr(w_out), _ptr(b_out), stride, V1, H,
                        WIND_BF16 if w_out.dtype == torch.bfloat16 else WIND_F32)
+
+
+def _on(device):
+    """The device of a call as the current one."""
+    import torch
+
+    return torch.cuda.device(device) if device.index != torch.cuda.current_device() else contextlib.nullcontext()
 
 
 def _asked(grad, names):
@@ -59,28 +70,28 @@ def _row_loss(kind, h, w_out, b_out, labels, logits, temperature, weights, grad)
     import torch
 
     layer, grad = _layer(w_out, b_out), _asked(grad, ("h", "w", "b"))
-    V1, H = w_out.shape
+    (V1, H), device = w_out.shape, w_out.device
     if h.dim() != 2 or labels.dim() != (1 if kind == "label" else 2):
         raise ValueError("h must be [N, H], labels [N], teacher labels [N, K]")
     N = h.shape[0]
-    _take(h, "h", (N, H), w_out.dtype, w_out, dense=False)
+    _take(h, "h", (N, H), w_out.dtype, device, dense=False)
     K = 1 if kind == "label" else int(labels.shape[1])
-    _take(labels, "labels", (N,) if kind == "label" else (N, K), torch.int32, w_out)
-    _take(logits, "teacher_logits", (N, K), torch.float32, w_out)
-    _take(weights, "weights", (N,), torch.float32, w_out)
+    _take(labels, "labels", (N,) if kind == "label" else (N, K), torch.int32, device)
+    _take(logits, "teacher_logits", (N, K), torch.float32, device)
+    _take(weights, "weights", (N,), torch.float32, device)
     stride = int(h.stride(0)) if N > 1 else H
     if stride < H:
         raise ValueError("h's rows must not overlap")
     lib = load_library()
-    with torch.cuda.device(w_out.device):
+    with _on(device):
         size = C.c_size_t(0)
         _check(lib.wind_row_loss_workspace_bytes(C.byref(layer), N, K, 1 if grad else 0, C.byref(size)))
-        workspace = torch.empty(size.value, dtype=torch.uint8, device=h.device)
-        loss = torch.empty(N, dtype=torch.float32, device=h.device)
+        workspace = torch.empty(size.value, dtype=torch.uint8, device=device)
+        loss = torch.empty(N, dtype=torch.float32, device=device)
         out = {"h": (N, H), "w": (V1, H), "b": (V1,)}
-        out = {g: torch.empty(out[g], dtype=torch.float32 if g == "b" else w_out.dtype, device=h.device) for g in grad}
+        out = {g: torch.empty(out[g], dtype=torch.float32 if g == "b" else w_out.dtype, device=device) for g in grad}
         tail = (_ptr(weights), N, _ptr(loss), _ptr(out.get("h")), _ptr(out.get("w")), _ptr(out.get("b")), _ptr(workspace), size.value,
-                torch.cuda.current_stream().cuda_stream)
+                torch.cuda.current_stream(device).cuda_stream)
         if kind == "label":
             _check(lib.wind_label_loss(C.byref(layer), _ptr(h), stride, _ptr(labels), *tail))
         else:
@@ -108,26 +119,26 @@ def transducer_loss(e, p, w_out, b_out, labels, frames, label_counts, weights=No
     import torch
 
     layer, grad = _layer(w_out, b_out), _asked(grad, ("e", "p", "w", "b"))
-    V1, H = w_out.shape
+    (V1, H), device = w_out.shape, w_out.device
     if e.dim() != 3 or p.dim() != 3 or labels.dim() != 2 or p.shape[1] < 1:
         raise ValueError("e must be [B, T, H], p [B, U + 1, H] and labels [B, U]")
     B, T, U = int(e.shape[0]), int(e.shape[1]), int(p.shape[1]) - 1
-    _take(e, "e", (B, T, H), w_out.dtype, w_out, dense=False)
-    _take(p, "p", (B, U + 1, H), w_out.dtype, w_out, dense=False)
-    _take(labels, "labels", (B, U), torch.int32, w_out)
-    _take(frames, "frames", (B,), torch.int32, w_out)
-    _take(label_counts, "label_counts", (B,), torch.int32, w_out)
-    _take(weights, "weights", (B,), torch.float32, w_out)
+    _take(e, "e", (B, T, H), w_out.dtype, device, dense=False)
+    _take(p, "p", (B, U + 1, H), w_out.dtype, device, dense=False)
+    _take(labels, "labels", (B, U), torch.int32, device)
+    _take(frames, "frames", (B,), torch.int32, device)
+    _take(label_counts, "label_counts", (B,), torch.int32, device)
+    _take(weights, "weights", (B,), torch.float32, device)
     lib = load_library()
-    with torch.cuda.device(w_out.device):
+    with _on(device):
         size = C.c_size_t(0)
         _check(lib.wind_transducer_loss_workspace_bytes(C.byref(layer), B, T, U, 1 if grad else 0, C.byref(size)))
-        workspace = torch.empty(size.value, dtype=torch.uint8, device=e.device)
-        loss = torch.empty(B, dtype=torch.float32, device=e.device)
+        workspace = torch.empty(size.value, dtype=torch.uint8, device=device)
+        loss = torch.empty(B, dtype=torch.float32, device=device)
         out = {"e": (B, T, H), "p": (B, U + 1, H), "w": (V1, H), "b": (V1,)}
-        out = {g: torch.empty(out[g], dtype=torch.float32 if g == "b" else w_out.dtype, device=e.device) for g in grad}
+        out = {g: torch.empty(out[g], dtype=torch.float32 if g == "b" else w_out.dtype, device=device) for g in grad}
         _check(lib.wind_transducer_loss(C.byref(layer), _ptr(e), int(e.stride(0)), int(e.stride(1)), _ptr(p), int(p.stride(0)), int(p.stride(1)),
                                         _ptr(labels), _ptr(frames), _ptr(label_counts), _ptr(weights), B, T, U, _ptr(loss), _ptr(out.get("e")),
                                         _ptr(out.get("p")), _ptr(out.get("w")), _ptr(out.get("b")), _ptr(workspace), size.value,
-                                        torch.cuda.current_stream().cuda_stream))
+                                        torch.cuda.current_stream(device).cuda_stream))
     return (loss, *(out[g] for g in grad)) if grad else loss
