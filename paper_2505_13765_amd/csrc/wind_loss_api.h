@@ -48,6 +48,11 @@ constexpr int kLossJoinParts = 128;
 int loss_planes(int dtype) { return dtype == WIND_BF16 ? 1 : 3; }
 int lattice_planes(int dtype) { return dtype == WIND_BF16 ? 2 : 3; }
 
+// A last column of tiles with at most 64 columns takes a tile of that width (0.45 of the time), where it is one of few: V1 is often a multiple of 128 and
+// one for blank.  184000 rows of 1025 outputs over 640: 325 -> 299 us a chunk; with 33 columns of tiles the second form of tile in the kernel costs what
+// it saves, and more.
+bool loss_narrow(const LossShape &s, long long n) { return s.bn >= 128 && n % s.bn > 0 && n % s.bn <= 64 && n / s.bn <= 16; }
+
 struct LossPick { int shape, splits, bm, bn; };
 // Shape, and parts of the summed axis, of a product of m x n outputs over `slabs` slabs of 32: the least time of the fullest CU, where a tile costs
 // its operations, its start and its results, and parts cost the writing and reading of their sums.
@@ -59,9 +64,10 @@ LossPick loss_pick(int planes, long long m, long long n, long long slabs, bool s
   for (int t = 0; t < count; ++t) {
     const LossShape &s = shapes[t];
     const long long tiles = ((m + s.bm - 1) / s.bm) * ((n + s.bn - 1) / s.bn);
+    const double weight = loss_narrow(s, n) && !split ? tiles - 0.55 * ((m + s.bm - 1) / s.bm) : (double)tiles;
     for (int parts = 1; parts <= (split ? 64 : 1); ++parts) {
       if (parts > 1 && (slabs / parts < 8 || tiles * parts > 1024)) break;
-      const long long fullest = (tiles * parts + 255) / 256;
+      const double fullest = std::ceil(weight * parts / 256);
       const double tile = ((double)((slabs + parts - 1) / parts) * products + s.start) * s.bm * s.bn * 64 / (kLossRate * (split ? s.rate_dx : s.rate) * (fullest == 1 ? s.alone : 1.0));
       const double time = fullest * tile + (parts > 1 ? 1.0 + parts * (double)m * n * 8 / 4e6 : 0.0);
       if (time < least) {
@@ -84,6 +90,7 @@ struct LossPlan {
   LossPick x, z, w;                  // logits, dz, dW
   bool dw_direct, dz_direct;         // written by their products: one chunk and one part; one part
   int parts;                         // column blocks of a row
+  bool narrow;                       // loss_narrow of the logits' tiles
   bool join;                         // joined by the launch that makes them
   // offsets into the workspace
   size_t idx, state, count, ticket, wp, rows, label, value, coef, scale, lse2, logit, part, dx, colsum, dw, total;
@@ -106,8 +113,9 @@ void loss_plan(LossPlan &p) {
   p.x = loss_pick(p.pa, m, p.V1, p.hblk, false);
   p.z = loss_pick(p.pd, m, p.H, p.vblk, true);
   p.w = loss_pick(p.pd, p.V1, p.H, (m + 31) / 32, true);
-  p.parts = (p.V1 + p.x.bn / 2 - 1) / (p.x.bn / 2);
-  p.join = N * p.K <= kLossJoinEntries && p.parts <= kLossJoinParts;
+  p.parts = 2 * ((p.V1 + p.x.bn - 1) / p.x.bn);
+  p.narrow = loss_narrow((p.pd == 3 ? kLossShapesF32 : kLossShapes)[p.x.shape], p.V1);
+  p.join = !p.narrow && N * p.K <= kLossJoinEntries && p.parts <= kLossJoinParts;
   p.dw_direct = p.chunks == 1 && p.w.splits == 1;
   p.dz_direct = p.kind != kLossLattice && p.z.splits == 1;
   size_t at = 0;
@@ -262,8 +270,9 @@ void loss_stats(const LossRun &r, LossNodes nodes) {
   loss_with_tile(p.pa, p.x.shape, [&](auto t) {
     using T = decltype(t);
     const unsigned grid = loss_grid((p.R + T::BM - 1) / T::BM, g.ct);
-    if (p.join) loss_stats_kernel<T, true><<<grid, 256, 0, r.s>>>(g, r.chunk, r.layer->b, r.rows, nodes, ticket);
-    else loss_stats_kernel<T, false><<<grid, 256, 0, r.s>>>(g, r.chunk, r.layer->b, r.rows, nodes, ticket);
+    if (p.join) loss_stats_kernel<T, true, false><<<grid, 256, 0, r.s>>>(g, r.chunk, r.layer->b, r.rows, nodes, ticket);
+    else if (T::NI > 1 && p.narrow) loss_stats_kernel<T, false, (T::NI > 1)><<<grid, 256, 0, r.s>>>(g, r.chunk, r.layer->b, r.rows, nodes, ticket);
+    else loss_stats_kernel<T, false, false><<<grid, 256, 0, r.s>>>(g, r.chunk, r.layer->b, r.rows, nodes, ticket);
   });
   if (p.join) return;
   if (p.parts > 256 && p.R <= 4096) loss_rows_done_kernel<4><<<p.R / 4, 256, 0, r.s>>>(r.rows, r.chunk, p.parts, nodes);
@@ -276,7 +285,9 @@ LossFinish loss_gradients(const LossRun &r, int chunk, bool dz, LossOut dz_out, 
   const LossDx d{r.at<bf16_t>(p.dx), (size_t)p.R * p.vblk * 32, p.pd, p.vblk, db ? r.at<float>(p.colsum) : nullptr};
   loss_with_tile(p.pa, p.x.shape, [&](auto t) {
     using T = decltype(t);
-    loss_dx_kernel<T><<<loss_grid((p.R + T::BM - 1) / T::BM, g.ct), 256, 0, r.s>>>(g, r.chunk, r.layer->b, d);
+    const unsigned grid = loss_grid((p.R + T::BM - 1) / T::BM, g.ct);
+    if (T::NI > 1 && p.narrow) loss_dx_kernel<T, (T::NI > 1)><<<grid, 256, 0, r.s>>>(g, r.chunk, r.layer->b, d);
+    else loss_dx_kernel<T, false><<<grid, 256, 0, r.s>>>(g, r.chunk, r.layer->b, d);
   });
   LossFinish f{};
   if (db) {
@@ -550,7 +561,7 @@ int wind_transducer_loss(const wind_output_layer *layer, const void *e, int64_t 
     r.chunk.c0 = c * p.R;
     lattice_chunk_kernel<<<dim3((unsigned)(p.R / 64), across), 256, 0, s>>>(l, r.chunk, z);
   };
-  for (int c = 0; c < p.chunks; ++c) {
+  for (int c = p.chunks - 1; c >= 0; --c) {   // the first chunk last: its rows are then there when the gradient begins with it
     if (!small) rows_of_chunk(c);
     loss_stats(r, l.nodes);
   }
@@ -570,7 +581,7 @@ int wind_transducer_loss(const wind_output_layer *layer, const void *e, int64_t 
     }
     const int columns = (p.hd + 255) / 256, n_e = fold.out[0] ? B * T * columns : 0, n_p = fold.out[1] ? B * (U + 1) * columns : 0;
     for (int c = 0; c < p.chunks; ++c) {
-      if (!whole) rows_of_chunk(c);   // (a single chunk's are still there)
+      if (c > 0) rows_of_chunk(c);
       lattice_counts_kernel<<<p.R / 256, 256, 0, s>>>(l, r.chunk);
       const LossFinish f = loss_gradients(r, c, n_e + n_p > 0, LossOut{}, dw, db);
       const int blocks = f.n_db + f.n_dw + n_e + n_p;

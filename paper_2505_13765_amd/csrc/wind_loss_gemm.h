@@ -45,6 +45,7 @@ struct LossTile {
   static constexpr int SMEM = RING > TILE ? RING : TILE;
   static constexpr int LS = PA_ * MI_ + PB_ * NI_, L = KPS_ * LS;   // loads per wave and slab, and stage
   static constexpr int PAIRS = PA_ == 3 && PB_ == 3 ? 6 : PA_ * PB_;
+  using Narrow = LossTile<MI_, 1, PA_, PB_, KPS_, S_, W_>;   // for a last column of tiles of at most 64 columns
   static_assert(PAIRS == 6 || PB_ == 1, "products of planes");
   static_assert(W_ * SMEM <= 160 * 1024 && (S_ - 1) * L < 64 && S_ >= 2, "LDS, vmcnt range");
 };

@@ -527,20 +527,16 @@ __global__ __launch_bounds__(256) void loss_rows_done_kernel(LossRowsDev r, Loss
   if ((int)blockIdx.x * ROWS < live) loss_rows_done<ROWS, false>(r, k, live, parts, nodes, (int)blockIdx.x * ROWS, sm);
 }
 
-// Row statistics.  JOIN: the last workgroup of a row tile (by a ticket, zero at launch) joins its column blocks itself; few rows and column blocks,
+// Row statistics.  NARROW: the last column of tiles has at most 64 columns and takes a tile of that width.  JOIN: the last workgroup of a row tile (by a ticket, zero at launch) joins its column blocks itself; few rows and column blocks,
 // where a launch of its own costs more.
 template <class T, bool JOIN>
-__global__ __launch_bounds__(256, T::W) void loss_stats_kernel(LossProduct g, LossChunk k, const float *bias, LossRowsDev r, LossNodes nodes, unsigned *ticket) {
-  __shared__ __attribute__((aligned(256))) unsigned char smem[T::SMEM];
-  const int live = chunk_rows(k);
-  int ti, tj, split;
-  if (!loss_place((int)blockIdx.x, (live + T::BM - 1) / T::BM, g.ct, 1, ti, tj, split)) return;
+__device__ __forceinline__ void loss_stats(const LossProduct &g, const LossChunk &k, const float *bias, int row0, int j0, int part0, unsigned char *smem) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  const int col0 = tj * T::BN + (wave & 1) * 32 * T::NI;
-  const int i0 = ti * T::BM + (wave >> 1) * 32 * T::MI + (lane & 31);
+  const int col0 = j0 + (wave & 1) * 32 * T::NI, part = part0 + (wave & 1);
+  const int i0 = row0 + (wave >> 1) * 32 * T::MI + (lane & 31);
   f32x16 acc[T::MI][T::NI];
   LossEntries<T> entries;
-  loss_mainloop<T, false, false>(g.a, g.b, ti * T::BM, tj * T::BN, 0, g.slabs, smem, acc, [&]() {
+  loss_mainloop<T, false, false>(g.a, g.b, row0, j0, 0, g.slabs, smem, acc, [&]() {
     entries.load(k, i0, col0);
     loss_bias<T>(bias, g.cols, col0, acc);
   });
@@ -561,8 +557,8 @@ __global__ __launch_bounds__(256, T::W) void loss_stats_kernel(LossProduct g, Lo
 #pragma unroll
       for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[mi][ni][r], k.c, -ref));
     sum += xor32_f32(sum);
-    if (lane < 32 && col0 < g.cols)
-      loss_leave<JOIN>(reinterpret_cast<unsigned long long *>(k.part) + (size_t)(col0 / (32 * T::NI)) * k.R + i,
+    if (lane < 32)
+      loss_leave<JOIN>(reinterpret_cast<unsigned long long *>(k.part) + (size_t)part * k.R + i,
                        __builtin_bit_cast(unsigned long long, make_float2(mc, sum)));
     if (entries.hit >> mi & 1u) {
       loss_tile_out<T>(acc[mi], tile);
@@ -579,6 +575,15 @@ __global__ __launch_bounds__(256, T::W) void loss_stats_kernel(LossProduct g, Lo
       __builtin_amdgcn_wave_barrier();
     }
   }
+}
+template <class T, bool JOIN, bool NARROW>
+__global__ __launch_bounds__(256, T::W) void loss_stats_kernel(LossProduct g, LossChunk k, const float *bias, LossRowsDev r, LossNodes nodes, unsigned *ticket) {
+  __shared__ __attribute__((aligned(256))) unsigned char smem[T::SMEM];
+  const int live = chunk_rows(k);
+  int ti, tj, split;
+  if (!loss_place((int)blockIdx.x, (live + T::BM - 1) / T::BM, g.ct, 1, ti, tj, split)) return;
+  if (NARROW && tj + 1 == g.ct) loss_stats<typename T::Narrow, JOIN>(g, k, bias, ti * T::BM, tj * T::BN, 2 * tj, smem);
+  else loss_stats<T, JOIN>(g, k, bias, ti * T::BM, tj * T::BN, 2 * tj, smem);
   if (!JOIN) return;
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // what this wave leaves has arrived
   int &last = *reinterpret_cast<int *>(smem + 4096);
@@ -586,7 +591,7 @@ __global__ __launch_bounds__(256, T::W) void loss_stats_kernel(LossProduct g, Lo
   if (threadIdx.x == 0) last = __hip_atomic_fetch_add(ticket + ti, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)g.ct - 1u;
   __syncthreads();
   if (!last) return;
-  const int end = min(live, (ti + 1) * T::BM), parts = (g.cols + 32 * T::NI - 1) / (32 * T::NI);
+  const int end = min(live, (ti + 1) * T::BM), parts = 2 * g.ct;
   float *const sm = reinterpret_cast<float *>(smem);
   if (end - ti * T::BM <= 16) loss_rows_done<16, true>(r, k, end, parts, nodes, ti * T::BM, sm);
   else
@@ -602,17 +607,13 @@ struct LossDx {
 };
 
 template <class T>
-__global__ __launch_bounds__(256, T::W) void loss_dx_kernel(LossProduct g, LossChunk k, const float *bias, LossDx d) {
-  __shared__ __attribute__((aligned(256))) unsigned char smem[T::SMEM];
-  const int live = chunk_rows(k);
-  int ti, tj, split;
-  if (!loss_place((int)blockIdx.x, (live + T::BM - 1) / T::BM, g.ct, 1, ti, tj, split)) return;
+__device__ __forceinline__ void loss_dx(const LossProduct &g, const LossChunk &k, const float *bias, const LossDx &d, int row0, int j0, unsigned char *smem) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), half = lane >> 5;
-  const int col0 = tj * T::BN + (wave & 1) * 32 * T::NI;
-  const int i0 = ti * T::BM + (wave >> 1) * 32 * T::MI + (lane & 31);
+  const int col0 = j0 + (wave & 1) * 32 * T::NI;
+  const int i0 = row0 + (wave >> 1) * 32 * T::MI + (lane & 31);
   f32x16 acc[T::MI][T::NI];
   LossEntries<T> entries;
-  loss_mainloop<T, false, false>(g.a, g.b, ti * T::BM, tj * T::BN, 0, g.slabs, smem, acc, [&]() {
+  loss_mainloop<T, false, false>(g.a, g.b, row0, j0, 0, g.slabs, smem, acc, [&]() {
     entries.load(k, i0, col0);
     loss_bias<T>(bias, g.cols, col0, acc);
   });
@@ -705,12 +706,22 @@ __global__ __launch_bounds__(256, T::W) void loss_dx_kernel(LossProduct g, LossC
       v = __uint_as_float(o[0]) + __uint_as_float(o[1]);
       if ((lane & 31) == (ni & 1) * 16 + r) keep[ni >> 1] = v;
     }
-  float *out = d.colsum + (size_t)(2 * ti + (wave >> 1)) * d.blocks * 32;
+  float *out = d.colsum + (size_t)(2 * (row0 / T::BM) + (wave >> 1)) * d.blocks * 32;
 #pragma unroll
   for (int j = 0; j < (T::NI + 1) / 2; ++j) {
     const int ni = 2 * j + ((lane & 31) >> 4), r = lane & 15, v = col0 + 32 * ni + 8 * (r >> 2) + 4 * half + (r & 3);
     if (ni < T::NI && v < d.blocks * 32) out[v] = keep[j];
   }
+}
+
+template <class T, bool NARROW>
+__global__ __launch_bounds__(256, T::W) void loss_dx_kernel(LossProduct g, LossChunk k, const float *bias, LossDx d) {
+  __shared__ __attribute__((aligned(256))) unsigned char smem[T::SMEM];
+  const int live = chunk_rows(k);
+  int ti, tj, split;
+  if (!loss_place((int)blockIdx.x, (live + T::BM - 1) / T::BM, g.ct, 1, ti, tj, split)) return;
+  if (NARROW && tj + 1 == g.ct) loss_dx<typename T::Narrow>(g, k, bias, d, ti * T::BM, tj * T::BN, smem);
+  else loss_dx<T>(g, k, bias, d, ti * T::BM, tj * T::BN, smem);
 }
 
 // ---- products of dx -----------------------------------------------------------------------------
