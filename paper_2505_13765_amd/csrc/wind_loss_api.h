@@ -363,7 +363,7 @@ int loss_rows_call(const char *name, const wind_output_layer *layer, const void 
   k.blocks = p.hblk;
   k.planes = p.pa;
   LossOut dz{dh, (size_t)p.H, p.dtype, p.H, nullptr, 0, 1, 0};
-  const bool small = p.chunks == 1 && N <= kLossSmallRows && N * p.K <= kLossSmall;
+  const bool small = p.chunks == 1 && N * p.K <= kLossSmall;
   if (small) {
     const unsigned across = std::min<unsigned>((unsigned)p.hblk, std::max(1u, 512u / (unsigned)(p.R / 64)));
     loss_small_kernel<<<w_blocks + (unsigned)(p.R / 64) * across, 256, 0, s>>>(w, (int)w_blocks, rows, k, r.chunk, (int)across, dh, r.at<unsigned>(p.ticket), p.R / 64);

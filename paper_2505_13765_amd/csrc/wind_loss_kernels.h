@@ -61,9 +61,20 @@ __device__ __forceinline__ float group_sum(float v, int group) {
   return v;
 }
 
+// A wave clears a row of the gradient.
+__device__ __forceinline__ void loss_clear_row(void *dh, size_t n, int dtype, int H) {
+  const size_t bytes = (size_t)H * (dtype ? 2 : 4);
+  char *row = (char *)dh + n * bytes;
+  for (size_t c = (threadIdx.x & 63) * 16; c < bytes; c += 1024) {
+    if (c + 16 <= bytes) store_any(row + c, u32x4{0u, 0u, 0u, 0u});
+    else
+      for (size_t x = c; x < bytes; x += 2) *reinterpret_cast<uint16_t *>(row + x) = 0;
+  }
+}
+
 // Which rows count: state 1, else 0 and the row's loss (0, or NaN if it names an output that does not exist) and gradient (zeros).
 __device__ __forceinline__ void loss_states(const LossRowsDev &r, int block, int nblocks, void *dh, int dtype, int H) {
-  const int lane = threadIdx.x & 63, group = r.kind == kLossLabel ? 1 : loss_group(r.K), rows = 256 / group;
+  const int group = r.kind == kLossLabel ? 1 : loss_group(r.K), rows = 256 / group;
   const int l = threadIdx.x & (group - 1);
   for (long long n0 = (long long)block * rows; n0 < r.N; n0 += (long long)nblocks * rows) {
     const long long n = n0 + threadIdx.x / group;
@@ -88,13 +99,7 @@ __device__ __forceinline__ void loss_states(const LossRowsDev &r, int block, int
     while (out) {
       const int at = __builtin_ctzll(out);
       out &= out - 1;
-      const size_t bytes = (size_t)H * (dtype ? 2 : 4);
-      char *row = (char *)dh + (size_t)(n0 + ((threadIdx.x & ~63) + at) / group) * bytes;
-      for (size_t c = lane * 16; c < bytes; c += 1024) {
-        if (c + 16 <= bytes) store_any(row + c, u32x4{0u, 0u, 0u, 0u});
-        else
-          for (size_t x = c; x < bytes; x += 2) *reinterpret_cast<uint16_t *>(row + x) = 0;
-      }
+      loss_clear_row(dh, (size_t)(n0 + ((threadIdx.x & ~63) + at) / group), dtype, H);
     }
   }
 }
@@ -280,10 +285,10 @@ __global__ __launch_bounds__(256) void loss_chunk_kernel(LossPack h, int pack_bl
 
 // Few rows, in one launch: W into panels, which rows count, and the rows' panels and entries.  Every workgroup of rows looks at all labels itself
 // (kLossSmall of them at most) and finds the places of its 64 rows among those that count; `across` of them share the 64 rows' panels.
-constexpr int kLossSmall = 16384, kLossSmallRows = 4096;
+constexpr int kLossSmall = 16384;
 __global__ __launch_bounds__(256) void loss_small_kernel(LossPack w, int w_blocks, LossRowsDev r, LossPack h, LossChunk k, int across, void *dh, unsigned *ticket,
                                                          int tickets) {
-  __shared__ unsigned char state[kLossSmallRows];
+  __shared__ __attribute__((aligned(16))) unsigned char state[kLossSmall];
   __shared__ int sums[4];
   if ((int)blockIdx.x < w_blocks) {
     loss_pack(w, (int)blockIdx.x, w_blocks);
@@ -293,33 +298,52 @@ __global__ __launch_bounds__(256) void loss_small_kernel(LossPack w, int w_block
   if (block == 0)
     for (int i = tid; i < tickets; i += 256) ticket[i] = 0u;
   // states of all rows; of the block's own source rows also what does not count
-  for (int n = tid; n < kLossSmallRows; n += 256) state[n] = 0;
-  __syncthreads();
-  const int group = r.kind == kLossLabel ? 1 : loss_group(r.K), rows = 256 / group, l = tid & (group - 1);
-  for (int n0 = 0; n0 < r.N; n0 += rows) {
-    const int n = n0 + tid / group;
-    bool some = false, wrong = false;
-    if (n < r.N)
-      for (int e = l; e < r.K; e += group) {
-        const int y = r.labels[(size_t)n * r.K + e];
-        wrong |= y >= r.V1;
-        some |= y >= 0 && (r.kind == kLossLabel || r.logits[(size_t)n * r.K + e] != -__builtin_inff());
-      }
-    for (int d = 1; d < group; d <<= 1) {
-      some |= __shfl_xor((int)some, d) != 0;
-      wrong |= __shfl_xor((int)wrong, d) != 0;
+  const int each = (r.N + 4095) / 4096 * 16;   // rows a thread looks at for their places, in sixteens
+  for (int n = r.N + tid; n < each * 256; n += 256) state[n] = 0;
+  auto settle = [&](int n, bool counts, bool wrong) {
+    state[n] = counts;
+    if (part == 0 && n >= i0 && n < i0 + 64 && !counts) r.loss[n] = wrong ? __builtin_nanf("") : 0.f;
+  };
+  if (r.kind == kLossLabel) {
+#pragma unroll 2
+    for (int n0 = tid * 4; n0 < r.N; n0 += 1024) {
+      i32x4 y = {-1, -1, -1, -1};
+      if (n0 + 4 <= r.N) y = load_any<i32x4>(r.labels + n0);
+      else
+        for (int j = 0; n0 + j < r.N; ++j) y[j] = r.labels[n0 + j];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (n0 + j < r.N) settle(n0 + j, y[j] >= 0 && y[j] < r.V1, y[j] >= r.V1);
     }
-    if (n >= r.N || l) continue;
-    state[n] = some && !wrong;
-    if (part == 0 && n >= i0 && n < i0 + 64 && !(some && !wrong)) r.loss[n] = wrong ? __builtin_nanf("") : 0.f;
+  } else {
+    const int group = loss_group(r.K), rows = 256 / group, l = tid & (group - 1);
+    for (int n0 = 0; n0 < r.N; n0 += rows) {
+      const int n = n0 + tid / group;
+      bool some = false, wrong = false;
+      if (n < r.N)
+        for (int e = l; e < r.K; e += group) {
+          const int y = r.labels[(size_t)n * r.K + e];
+          wrong |= y >= r.V1;
+          some |= y >= 0 && r.logits[(size_t)n * r.K + e] != -__builtin_inff();
+        }
+      for (int d = 1; d < group; d <<= 1) {
+        some |= __shfl_xor((int)some, d) != 0;
+        wrong |= __shfl_xor((int)wrong, d) != 0;
+      }
+      if (n < r.N && l == 0) settle(n, some && !wrong, wrong);
+    }
   }
   __syncthreads();
-  // 16 rows a thread: their places
-  uint32_t bits = 0;
-  const u32x4 st = *reinterpret_cast<const u32x4 *>(state + tid * 16);
+  // the places of a thread's rows
+  auto bits_of = [&](int i) {
+    const u32x4 st = *reinterpret_cast<const u32x4 *>(state + tid * each + i);
+    uint32_t bits = 0;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) bits |= ((st[i >> 2] >> (8 * (i & 3))) & 1u) << i;
-  const int mine = __popc(bits);
+    for (int j = 0; j < 16; ++j) bits |= ((st[j >> 2] >> (8 * (j & 3))) & 1u) << j;
+    return bits;
+  };
+  int mine = 0;
+  for (int i = 0; i < each; i += 16) mine += __popc(bits_of(i));
   int sum = mine;
   for (int d = 1; d < 64; d <<= 1) {
     const int o = __shfl_up(sum, d);
@@ -333,11 +357,10 @@ __global__ __launch_bounds__(256) void loss_small_kernel(LossPack w, int w_block
     live += sums[w2];
   }
   if (block == 0 && tid == 0) *r.count = live;
-  while (bits) {   // (the blocks of the same rows write the same)
-    if (put >= i0 && put < i0 + 64) r.idx[put] = tid * 16 + __builtin_ctz(bits);
-    ++put;
-    bits &= bits - 1;
-  }
+  if (put < i0 + 64 && put + mine > i0)
+    for (int i = 0; i < each; i += 16)
+      for (uint32_t bits = bits_of(i); bits; bits &= bits - 1, ++put)   // (the blocks of the same rows write the same)
+        if (put >= i0 && put < i0 + 64) r.idx[put] = tid * each + i + __builtin_ctz(bits);
   __syncthreads();
   const int used = min((live + 255) & ~255, k.R);
   if (part == 0) loss_entries(r, k, live, i0, min(i0 + 64, used), 1);
@@ -354,10 +377,7 @@ __global__ __launch_bounds__(256) void loss_small_kernel(LossPack w, int w_block
   if (!dh) return;
   for (int n = i0 + wave + 4 * part; n < min(i0 + 64, r.N); n += 4 * across) {   // gradients of rows that do not count
     if (state[n]) continue;
-    for (int c = lane; c < h.cols; c += 64) {
-      if (h.dtype) ((bf16_t *)dh)[(size_t)n * h.cols + c] = 0;
-      else ((float *)dh)[(size_t)n * h.cols + c] = 0.f;
-    }
+    loss_clear_row(dh, n, h.dtype, h.cols);
   }
 }
 
