@@ -415,7 +415,7 @@ int wind_transducer_loss_workspace_bytes(const wind_output_layer *layer, int B, 
  *               frames is left out (loss 0, no gradient); one with a label that does not exist is left out and its loss is NaN; one of probability zero
  *               has loss +inf and no gradient
  *   loss        DEVICE [B] fp32;  de [B, T, H], dp [B, U + 1, H] (zeros beyond frames and label_counts), dw [V1, H], db [V1]
- * U <= 4095, T * (U + 1) < 2^27, B * T * (U + 1) < 2^31 and B * (T + U + 1) * H / 256 < 2^31 (WIND_ERR_UNSUPPORTED).
+ * U <= 4095, T * (U + 1) < 2^27, B * T * (U + 1) < 2^31 and B * (T + U + 1) * H / 64 < 2^31 (WIND_ERR_UNSUPPORTED).
  */
 int wind_transducer_loss(const wind_output_layer *layer, const void *e, int64_t e_stride_b, int64_t e_stride_t, const void *p, int64_t p_stride_b,
                          int64_t p_stride_u, const int32_t *labels, const int32_t *frames, const int32_t *label_counts, const float *weights, int B, int T,

@@ -41,8 +41,15 @@ constexpr size_t kLossChunkBytes = 1200u << 20;
 constexpr int kLossMaxEntries = 1024;
 // Entries (of all rows) and column blocks up to which a row tile's last workgroup joins its column blocks: one launch less, 36 -> 31 us for 16 rows of 1025
 // outputs.  With more, that workgroup is what the others' results wait for (3001 rows of 64 entries: 73 us against 51 and 6).
+// Entries x column blocks from which entries are sorted by column block: a launch of 6 to 8 us against every tile looking at all of its rows' entries (12000 rows,
+// 16 entries, 130 blocks: 838 -> 788 us a step; 3476, 23, 112, fp32 losses: 143 -> 137; 3001, 64, 18: even).
+constexpr double kLossSortWork = 4e6;
 constexpr long long kLossJoinEntries = 4096;
 constexpr int kLossJoinParts = 128;
+// Sums of dz that 16 threads share instead of 4: of at least kLatticeLong rows, where 4 would leave the chip short of workgroups (240 frames of 2 labels, 24
+// utterances: 56 us for 96 of them; with thousands, 750 frames of 121, 16 threads cost 6 % of the whole step).
+constexpr int kLatticeLong = 64;
+constexpr long long kLatticeFew = 1024;
 
 // the bf16 planes that make up a stored value of each type, and the sum of two bf16 values (hidden rows of the lattice)
 int loss_planes(int dtype) { return dtype == WIND_BF16 ? 1 : 3; }
@@ -91,9 +98,10 @@ struct LossPlan {
   bool dw_direct, dz_direct;         // written by their products: one chunk and one part; one part
   int parts;                         // column blocks of a row
   bool narrow;                       // loss_narrow of the logits' tiles
+  bool sort;                         // entries sorted by column block
   bool join;                         // joined by the launch that makes them
   // offsets into the workspace
-  size_t idx, state, count, ticket, wp, rows, label, value, coef, scale, lse2, logit, part, dx, colsum, dw, total;
+  size_t idx, state, count, ticket, wp, rows, label, value, coef, scale, lse2, logit, part, sorted, begin, dx, colsum, dw, total;
   size_t off, place, tb, ub, slot, arcs, nlse2, alpha, beta, dz, de, dp;
 };
 
@@ -115,7 +123,8 @@ void loss_plan(LossPlan &p) {
   p.w = loss_pick(p.pd, p.V1, p.H, (m + 31) / 32, true);
   p.parts = 2 * ((p.V1 + p.x.bn - 1) / p.x.bn);
   p.narrow = loss_narrow((p.pd == 3 ? kLossShapesF32 : kLossShapes)[p.x.shape], p.V1);
-  p.join = !p.narrow && N * p.K <= kLossJoinEntries && p.parts <= kLossJoinParts;
+  p.sort = p.kind == kLossDistill && p.K > 2 && p.K <= kLossSortMost && N * p.K > kLossSmall && (double)N * p.K * p.parts >= kLossSortWork;
+  p.join = !p.narrow && !p.sort && N * p.K <= kLossJoinEntries && p.parts <= kLossJoinParts;
   p.dw_direct = p.chunks == 1 && p.w.splits == 1;
   p.dz_direct = p.kind != kLossLattice && p.z.splits == 1;
   size_t at = 0;
@@ -135,6 +144,10 @@ void loss_plan(LossPlan &p) {
   p.scale = take(R * 4);
   p.lse2 = take(R * 4);
   p.part = take(R * 8 * p.parts);
+  if (p.sort) {
+    p.sorted = take(R * p.K * 4);
+    p.begin = take(R / 32 * ((size_t)p.parts + 1) * 4);
+  }
   if (p.kind != kLossLattice) {
     p.idx = take(n * 4);
     p.state = take(n);
@@ -211,8 +224,10 @@ void loss_with_tile(int pa, int shape, F &&f) {
 // products of dx: no sums of two values among them
 template <class F>
 void loss_with_dx_tile(int pd, int shape, F &&f) {
-  if (pd == 3) loss_with_tile(3, shape, f);
-  else if (shape == 0) f(LossTiles<1, 1>::T0{});
+  if (pd == 3) {
+    if (shape == 0) f(LossTiles<3, 3>::T0{});
+    else f(LossTiles<3, 3>::T1{});
+  } else if (shape == 0) f(LossTiles<1, 1>::T0{});
   else if (shape == 1) f(LossTiles<1, 1>::T1{});
   else if (shape == 2) f(LossTiles<1, 1>::T2{});
   else f(LossTiles<1, 1>::T3{});
@@ -246,6 +261,11 @@ LossPack loss_begin(LossRun &r) {
   k.lse2 = r.at<float>(p.lse2);
   k.logit = r.at<float>(p.logit);
   k.part = r.at<float2>(p.part);
+  k.parts = p.parts;
+  if (p.sort) {
+    k.sorted = r.at<uint32_t>(p.sorted);
+    k.begin = r.at<int>(p.begin);
+  }
   k.c = kLog2e * r.rows.inv_tau;
   const wind_output_layer &l = *r.layer;
   LossPack w{};
@@ -376,6 +396,7 @@ int loss_rows_call(const char *name, const wind_output_layer *layer, const void 
     k.c0 = r.chunk.c0 = c * p.R;
     const unsigned packs = loss_blocks((size_t)p.R * p.hblk * 4), entries = loss_blocks((size_t)p.R * std::min(p.K, 64), 256, 1024);
     if (!small) loss_chunk_kernel<<<packs + entries, 256, 0, s>>>(k, (int)packs, rows, r.chunk);
+    if (p.sort) loss_sort_kernel<<<p.R / 32, 256, 0, s>>>(r.chunk, LossBlocks{p.x.bn, (p.V1 + p.x.bn - 1) / p.x.bn, p.narrow});
     loss_stats(r, LossNodes{});
     if (!p.grads) continue;
     dz.idx = rows.idx + k.c0;
@@ -403,7 +424,7 @@ int lattice_plan(LossPlan &p, const wind_output_layer *layer, int B, int T, int 
   if (B < 1 || T < 0 || U < 0) return fail(WIND_ERR_ARG, "B >= 1, T >= 0 and U >= 0 required");
   if (U > 4095) return fail(WIND_ERR_UNSUPPORTED, "U must be at most 4095");
   if ((double)T * (U + 1.0) >= 134217728.0) return fail(WIND_ERR_UNSUPPORTED, "T * (U + 1) must be below 2^27");
-  if ((double)B * T * (U + 1.0) >= 2147483648.0 || (double)B * ((double)T + U + 1.0) * ((layer->H + 255) / 256) >= 2147483648.0) return fail(WIND_ERR_UNSUPPORTED, "B * T * (U + 1) and B * (T + U + 1) * H / 256 must be below 2^31");
+  if ((double)B * T * (U + 1.0) >= 2147483648.0 || (double)B * ((double)T + U + 1.0) * ((layer->H + 63) / 64) >= 2147483648.0) return fail(WIND_ERR_UNSUPPORTED, "B * T * (U + 1) and B * (T + U + 1) * H / 64 must be below 2^31");
   p.kind = kLossLattice;
   p.dtype = layer->dtype;
   p.V1 = layer->V1;
@@ -574,12 +595,16 @@ int wind_transducer_loss(const wind_output_layer *layer, const void *e, int64_t 
   else lattice_sums_kernel<4, 1, true><<<runs, (unsigned)round_up((size_t)(cells + 3) / 4, 64), 0, s>>>(l, both);
   if (p.grads) {
     const bool whole = p.chunks == 1;
-    LatticeFold fold{r.at<float>(p.dz), p.hd, p.z.splits, (size_t)p.R * p.hd, {nullptr, nullptr}, {T ? de : nullptr, dp}};
+    LatticeFold fold{r.at<float>(p.dz), p.hd, p.z.splits, (size_t)p.R * p.hd, {nullptr, nullptr}, {T ? de : nullptr, dp}, {0, 0}};
+    const long long over = (p.hd + 255) / 256;
+    fold.wide[0] = U + 1 >= kLatticeLong && over * B * T <= kLatticeFew ? 64 : 256;
+    fold.wide[1] = T >= kLatticeLong && over * B * (U + 1) <= kLatticeFew ? 64 : 256;
     if (!whole) {
       fold.sum[0] = r.at<float>(p.de);
       fold.sum[1] = r.at<float>(p.dp);
     }
-    const int columns = (p.hd + 255) / 256, n_e = fold.out[0] ? B * T * columns : 0, n_p = fold.out[1] ? B * (U + 1) * columns : 0;
+    auto columns = [&](int which) { return (p.hd + fold.wide[which] - 1) / fold.wide[which]; };
+    const int n_e = fold.out[0] ? B * T * columns(0) : 0, n_p = fold.out[1] ? B * (U + 1) * columns(1) : 0;
     for (int c = 0; c < p.chunks; ++c) {
       if (c > 0) rows_of_chunk(c);
       lattice_counts_kernel<<<p.R / 256, 256, 0, s>>>(l, r.chunk);

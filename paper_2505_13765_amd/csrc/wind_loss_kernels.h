@@ -228,6 +228,10 @@ struct LossChunk {
   float *lse2;                 // [R] (+inf: row does not count)
   float *logit;                // [K][R] the entries' logits
   float2 *part;                // [column blocks][R] (largest, sum)
+  // many entries (else null): those of 32 rows by column block, and where each block's begin
+  uint32_t *sorted;            // [R / 32][32 K]: column within its block << 18 | row << 12 | entry
+  int *begin;                  // [R / 32][parts + 1]
+  int parts;
   float c;                     // log2(e) / tau
 };
 __device__ __forceinline__ int chunk_rows(const LossChunk &k) { return min(max(*k.count - k.c0, 0), k.R); }
@@ -281,6 +285,50 @@ __global__ __launch_bounds__(256) void loss_chunk_kernel(LossPack h, int pack_bl
   }
   const int live = chunk_rows(k), block = (int)blockIdx.x - pack_blocks, group = r.kind == kLossLabel ? 1 : loss_group(r.K);
   loss_entries(r, k, live, block * (256 / group), min((live + 255) & ~255, k.R), (int)gridDim.x - pack_blocks);
+}
+
+// Entries of 32 rows sorted by column block, column, row and entry, so that a tile of logits finds its own without looking at the others' and an output that a
+// row names again follows itself (39 entries a row over 10169 outputs: gradient of the logits 102 us, looking at all).  Bitonic, in LDS.
+constexpr int kLossSortMost = 128;     // entries a row
+struct LossBlocks { int bn, ct, narrow; };   // columns of a tile, tiles, and whether the last one is narrow: two blocks a tile
+__global__ __launch_bounds__(256) void loss_sort_kernel(LossChunk k, LossBlocks b) {
+  __shared__ unsigned long long key[32 * kLossSortMost];   // block << 32 | column << 18 | row << 12 | entry
+  const int rows0 = blockIdx.x * 32, tid = threadIdx.x, n = 32 * k.K;
+  if (rows0 >= ((chunk_rows(k) + 255) & ~255)) return;
+  int size = 64;
+  while (size < n) size <<= 1;
+  for (int x = tid; x < size; x += 256) {
+    const int row = x & 31, e = x >> 5, y = x < n ? k.label[(size_t)e * k.R + rows0 + row] : -1;
+    unsigned long long v = ~0ull;
+    if (y >= 0) {
+      const int tile = y / b.bn, width = b.narrow && tile + 1 == b.ct ? 32 : b.bn / 2, in = y - tile * b.bn, half = in / width;
+      v = (unsigned long long)(2 * tile + half) << 32 | (unsigned)((in - half * width) << 18 | row << 12 | e);
+    }
+    key[x] = v;
+  }
+  __syncthreads();
+  for (int run = 2; run <= size; run <<= 1)
+    for (int step = run >> 1; step > 0; step >>= 1) {
+      for (int t = tid; t < size / 2; t += 256) {
+        const int i = 2 * t - (t & (step - 1)), j = i + step;
+        const unsigned long long u = key[i], v = key[j];
+        if ((u > v) == ((i & run) == 0)) {
+          key[i] = v;
+          key[j] = u;
+        }
+      }
+      __syncthreads();
+    }
+  for (int x = tid; x < n; x += 256) k.sorted[(size_t)blockIdx.x * n + x] = (uint32_t)key[x];
+  for (int p = tid; p <= k.parts; p += 256) {   // the first key of block p or above
+    int lo = 0, hi = size;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if ((key[mid] >> 32) < (unsigned long long)p) lo = mid + 1;
+      else hi = mid;
+    }
+    k.begin[(size_t)blockIdx.x * (k.parts + 1) + p] = min(lo, n);
+  }
 }
 
 // Few rows, in one launch: W into panels, which rows count, and the rows' panels and entries.  Every workgroup of rows looks at all labels itself
@@ -410,8 +458,20 @@ __device__ __forceinline__ void loss_tile_out(const f32x16 (&acc)[T::NI], float 
 template <class T>
 struct LossEntries {
   int label[T::MI][2];
+  int first[T::MI], end[T::MI];   // sorted entries of a block
   unsigned hit;
-  __device__ __forceinline__ void load(const LossChunk &k, int i0, int col0) {
+  __device__ __forceinline__ void load(const LossChunk &k, int i0, int col0, int part) {
+    if (k.sorted) {
+      hit = 0;
+#pragma unroll
+      for (int mi = 0; mi < T::MI; ++mi) {
+        const int *begin = k.begin + (size_t)(i0 / 32 + mi) * (k.parts + 1) + part;
+        first[mi] = __builtin_amdgcn_readfirstlane(begin[0]);
+        end[mi] = __builtin_amdgcn_readfirstlane(begin[1]);
+        hit |= end[mi] > first[mi] ? 1u << mi : 0u;
+      }
+      return;
+    }
     bool in[T::MI];
 #pragma unroll
     for (int mi = 0; mi < T::MI; ++mi) {
@@ -557,7 +617,7 @@ __device__ __forceinline__ void loss_stats(const LossProduct &g, const LossChunk
   f32x16 acc[T::MI][T::NI];
   LossEntries<T> entries;
   loss_mainloop<T, false, false>(g.a, g.b, row0, j0, 0, g.slabs, smem, acc, [&]() {
-    entries.load(k, i0, col0);
+    entries.load(k, i0, col0, part);
     loss_bias<T>(bias, g.cols, col0, acc);
   });
   float *tile = reinterpret_cast<float *>(smem) + wave * 32 * T::PITCH;
@@ -582,7 +642,14 @@ __device__ __forceinline__ void loss_stats(const LossProduct &g, const LossChunk
                        __builtin_bit_cast(unsigned long long, make_float2(mc, sum)));
     if (entries.hit >> mi & 1u) {
       loss_tile_out<T>(acc[mi], tile);
-      if (k.K <= 2) {   // a lane each
+      if (k.sorted) {
+        const uint32_t *list = k.sorted + (size_t)(i0 / 32 + mi) * 32 * k.K;
+        for (int x = entries.first[mi] + lane; x < entries.end[mi]; x += 64) {
+          const uint32_t w = list[x];
+          const int row = (int)(w >> 12) & 31, e = (int)(w & 4095u);
+          loss_leave<JOIN>(k.logit + (size_t)e * k.R + (i - (lane & 31)) + row, tile[row * T::PITCH + (int)(w >> 18)]);
+        }
+      } else if (k.K <= 2) {   // a lane each
         const int at = (lane < 32 ? entries.label[mi][0] : entries.label[mi][1]) - col0;
         if (entries.inside(at)) loss_leave<JOIN>(k.logit + (size_t)(lane >> 5) * k.R + i, tile[(lane & 31) * T::PITCH + at]);
       } else for (int e0 = 0; e0 < k.K; e0 += entries.kBatch) {
@@ -627,14 +694,14 @@ struct LossDx {
 };
 
 template <class T>
-__device__ __forceinline__ void loss_dx(const LossProduct &g, const LossChunk &k, const float *bias, const LossDx &d, int row0, int j0, unsigned char *smem) {
+__device__ __forceinline__ void loss_dx(const LossProduct &g, const LossChunk &k, const float *bias, const LossDx &d, int row0, int j0, int part0, unsigned char *smem) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), half = lane >> 5;
-  const int col0 = j0 + (wave & 1) * 32 * T::NI;
+  const int col0 = j0 + (wave & 1) * 32 * T::NI, part = part0 + (wave & 1);
   const int i0 = row0 + (wave >> 1) * 32 * T::MI + (lane & 31);
   f32x16 acc[T::MI][T::NI];
   LossEntries<T> entries;
   loss_mainloop<T, false, false>(g.a, g.b, row0, j0, 0, g.slabs, smem, acc, [&]() {
-    entries.load(k, i0, col0);
+    entries.load(k, i0, col0, part);
     loss_bias<T>(bias, g.cols, col0, acc);
   });
   float *tile = reinterpret_cast<float *>(smem) + wave * 32 * T::PITCH;
@@ -649,7 +716,22 @@ __device__ __forceinline__ void loss_dx(const LossProduct &g, const LossChunk &k
     if (entries.hit >> mi & 1u) {
       loss_tile_out<T>(acc[mi], tile);
       float *row = tile + (lane & 31) * T::PITCH;
-      if (k.K <= 2) {
+      if (k.sorted) {
+        const int n = entries.end[mi] - entries.first[mi];
+        const uint32_t *list = k.sorted + (size_t)(i0 / 32 + mi) * 32 * k.K + entries.first[mi];
+        const float *coef = k.coef + (i - (lane & 31));
+        for (int x = lane; x < n; x += 64) {   // the first of an output's entries takes all of them off, in order
+          const uint32_t w = list[x];
+          if (x > 0 && list[x - 1] >> 12 == w >> 12) continue;
+          const int row_x = (int)(w >> 12) & 31;
+          float &at = tile[row_x * T::PITCH + (int)(w >> 18)];
+          float v = at - coef[(size_t)(w & 4095u) * k.R + row_x];
+          for (int y = x + 1; y < n && list[y] >> 12 == w >> 12; ++y) v -= coef[(size_t)(list[y] & 4095u) * k.R + row_x];
+          at = v;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+      } else if (k.K <= 2) {
         const int at[2] = {entries.label[mi][0] - col0, entries.label[mi][1] - col0};
         const float c[2] = {k.coef[i], k.K > 1 ? k.coef[k.R + i] : 0.f};
         if (half == 0) {
@@ -740,8 +822,8 @@ __global__ __launch_bounds__(256, T::W) void loss_dx_kernel(LossProduct g, LossC
   const int live = chunk_rows(k);
   int ti, tj, split;
   if (!loss_place((int)blockIdx.x, (live + T::BM - 1) / T::BM, g.ct, 1, ti, tj, split)) return;
-  if (NARROW && tj + 1 == g.ct) loss_dx<typename T::Narrow>(g, k, bias, d, ti * T::BM, tj * T::BN, smem);
-  else loss_dx<T>(g, k, bias, d, ti * T::BM, tj * T::BN, smem);
+  if (NARROW && tj + 1 == g.ct) loss_dx<typename T::Narrow>(g, k, bias, d, ti * T::BM, tj * T::BN, 2 * tj, smem);
+  else loss_dx<T>(g, k, bias, d, ti * T::BM, tj * T::BN, 2 * tj, smem);
 }
 
 // ---- products of dx -----------------------------------------------------------------------------

@@ -314,8 +314,8 @@ __global__ __launch_bounds__(256) void lattice_counts_kernel(LatticeDev l, LossC
   k.lse2[i] = l.nodes.lse2[n];
 }
 
-// Sums of dz, where z is above zero, over the chunk's rows of one frame (which = 0) or of one prediction row (which = 1): a workgroup 256 columns,
-// its waves share the rows.  The whole lattice in one chunk: the sums are rounded and stored, rows that no utterance has as zeros.  Else the
+// Sums of dz, where z is above zero, over the chunk's rows of one frame (which = 0) or of one prediction row (which = 1): a workgroup takes 256 columns
+// with 4 threads each, or, for few long sums, 64 with 16.  The whole lattice in one chunk: the sums are rounded and stored, rows that no utterance has as zeros.  Else the
 // chunk that holds the first of a sum's rows writes, later ones add, and lattice_done_kernel rounds.
 struct LatticeFold {
   const float *dz;
@@ -323,6 +323,7 @@ struct LatticeFold {
   size_t part;
   float *sum[2];               // [B T, ld], [B (U + 1), ld], or null
   void *out[2];                // the gradients de, dp, or null
+  int wide[2];                 // columns of a workgroup: 256 or 64
 };
 __device__ __forceinline__ f32x4 lattice_load4(const LatticeDev &l, const char *row, int c) {
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
@@ -352,11 +353,13 @@ __device__ __forceinline__ void lattice_store4(const LatticeDev &l, void *out, s
     else ((float *)out)[row * l.H + c + j] = v[j];
   }
 }
+template <int WIDE>
 __device__ __forceinline__ void lattice_fold(const LatticeDev &l, const LossChunk &k, const LatticeFold &f, int which, int block) {
-  __shared__ f32x4 sums[4][64];
-  const int across = (f.ld + 255) / 256, row = block / across, per = which ? l.U + 1 : l.T;
+  __shared__ f32x4 sums[256];
+  constexpr int lanes = WIDE / 4, groups = 256 / lanes;
+  const int across = (f.ld + WIDE - 1) / WIDE, row = block / across, per = which ? l.U + 1 : l.T;
   const int live = chunk_rows(k), b = row / per, x = row - b * per;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (block - row * across) * 256 + lane * 4;
+  const int lane = threadIdx.x & (lanes - 1), wave = threadIdx.x / lanes, c = (block - row * across) * WIDE + lane * 4;
   const int T = l.tb[b], U1 = l.ub[b] + 1;
   const bool whole = f.sum[which] == nullptr;
   if (T == 0 || x >= (which ? U1 : T)) {
@@ -373,7 +376,7 @@ __device__ __forceinline__ void lattice_fold(const LatticeDev &l, const LossChun
   if (c < l.H) {
     const f32x4 own = lattice_load4(l, which ? lattice_p(l, b, x) : lattice_e(l, b, x), c);
 #pragma unroll 4
-    for (int j = j0 + wave; j < j1; j += 4) {
+    for (int j = j0 + wave; j < j1; j += groups) {
       const float *at = f.dz + (size_t)(first + j * step - k.c0) * f.ld + c;
       f32x4 v = *reinterpret_cast<const f32x4 *>(at);
       const f32x4 other = lattice_load4(l, which ? lattice_e(l, b, j) : lattice_p(l, b, j), c);
@@ -382,10 +385,11 @@ __device__ __forceinline__ void lattice_fold(const LatticeDev &l, const LossChun
       for (int i = 0; i < 4; ++i) s[i] += own[i] + other[i] > 0.f ? v[i] : 0.f;
     }
   }
-  sums[wave][lane] = s;
+  sums[threadIdx.x] = s;
   __syncthreads();
   if (wave || c >= l.H) return;
-  s = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+#pragma unroll
+  for (int q = 1; q < groups; ++q) s += sums[q * lanes + lane];
   if (whole) {
     lattice_store4(l, f.out[which], row, c, s);
     return;
@@ -397,7 +401,10 @@ __device__ __forceinline__ void lattice_fold(const LatticeDev &l, const LossChun
 __global__ __launch_bounds__(256) void lattice_finish_kernel(LossFinish f, LossChunk k, LatticeDev l, LatticeFold fold, int n_e) {
   int block = (int)blockIdx.x;
   if (loss_finish(f, k, block)) return;
-  lattice_fold(l, k, fold, block < n_e ? 0 : 1, block < n_e ? block : block - n_e);
+  const int which = block < n_e ? 0 : 1;
+  if (which) block -= n_e;
+  if (fold.wide[which] == 256) lattice_fold<256>(l, k, fold, which, block);
+  else lattice_fold<64>(l, k, fold, which, block);
 }
 
 // The sums of several chunks, rounded once; rows that no utterance has are zero.

@@ -65,6 +65,34 @@ def test_distill_loss(N, H, V1, K, tau, dtype):
     close(wind.distill_loss(h, w, b, labels, logits, tau), *ref["loss"], "loss alone")
 
 
+@pytest.mark.parametrize("N,H,V1,K,dtype", [(2500, 40, 9000, 24, "bf16"), (1500, 33, 8193, 40, "f32"), (900, 96, 8200, 128, "bf16"), (20000, 24, 70, 3, "bf16")])
+def test_many_teacher_logits(N, H, V1, K, dtype):
+    """Entries enough to be sorted by column, with outputs that a row names twice or in all of its entries."""
+    wind = api()
+    h, w, b, _, weights = rows(N, H, V1, dtype, N, left_out=0.0)
+    g = torch.Generator().manual_seed(N + 1)
+    labels = torch.randint(-1, V1, (N, K), generator=g, dtype=torch.int32)
+    labels[:, 1] = labels[:, 0]
+    labels[::7, 2] = labels[::7, 0]
+    labels[5] = V1 - 1
+    labels[6] = -1
+    logits = 2 * torch.randn((N, K), generator=g)
+    labels, logits = labels.cuda(), logits.cuda()
+    ref = row_loss(h, w, b, labels, logits, 2.0, weights)
+    got = wind.distill_loss(h, w, b, labels, logits, 2.0, weights, grad=("h", "w", "b"))
+    check(got, ref, "hwb")
+    again = wind.distill_loss(h, w, b, labels, logits, 2.0, weights, grad=("h", "w", "b"))
+    assert all(torch.equal(x, y) for x, y in zip(got, again))
+
+
+def test_many_short_rows():
+    """More rows than one launch counts, an odd number, most of them padding."""
+    wind = api()
+    h, w, b, labels, weights = rows(40961, 40, 50, "bf16", 15, left_out=0.7)
+    ref = row_loss(h, w, b, labels, weights=weights)
+    check(wind.label_loss(h, w, b, labels, weights, grad=("h", "w", "b")), ref, "hwb")
+
+
 @pytest.mark.parametrize("dtype", ("bf16", "f32"))
 def test_larger_tiles(dtype):
     """Shapes whose products take 128- and 256-wide tiles, ragged at every edge."""
@@ -157,7 +185,7 @@ GRAD = ("e", "p", "w", "b")
 
 @pytest.mark.parametrize("dtype", ("bf16", "f32"))
 @pytest.mark.parametrize("B,T,U,H,V1", [(1, 1, 0, 8, 2), (1, 1, 3, 8, 5), (2, 6, 0, 33, 9), (3, 9, 4, 64, 33), (5, 17, 11, 40, 70), (2, 3, 70, 32, 40), (70, 4, 3, 16, 12),
-                                        (2, 40, 130, 24, 31)])
+                                        (2, 40, 130, 24, 31), (3, 150, 5, 72, 1025), (40, 6, 30, 20, 17)])
 def test_transducer_loss(B, T, U, H, V1, dtype):
     wind = api()
     a = lattice(B, T, U, H, V1, dtype, B + T + U)
