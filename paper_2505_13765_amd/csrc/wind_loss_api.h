@@ -49,6 +49,7 @@ constexpr int kLossJoinParts = 128;
 // Sums of dz that 16 threads share instead of 4: of at least kLatticeLong rows, where 4 would leave the chip short of workgroups (240 frames of 2 labels, 24
 // utterances: 56 us for 96 of them; with thousands, 750 frames of 121, 16 threads cost 6 % of the whole step).
 constexpr int kLatticeLong = 64;
+constexpr long long kLatticeOnce = 64ll << 20;   // bytes of dz from which it is read once for both folds, at the price of a launch
 constexpr long long kLatticeFew = 1024;
 
 // the bf16 planes that make up a stored value of each type, and the sum of two bf16 values (hidden rows of the lattice)
@@ -98,11 +99,12 @@ struct LossPlan {
   bool dw_direct, dz_direct;         // written by their products: one chunk and one part; one part
   int parts;                         // column blocks of a row
   bool narrow;                       // loss_narrow of the logits' tiles
+  bool fold_once;                    // dz is read once for both of its folds
   bool sort;                         // entries sorted by column block
   bool join;                         // joined by the launch that makes them
   // offsets into the workspace
   size_t idx, state, count, ticket, wp, rows, label, value, coef, scale, lse2, logit, part, sorted, begin, dx, colsum, dw, total;
-  size_t off, place, tb, ub, slot, arcs, nlse2, alpha, beta, dz, de, dp;
+  size_t off, place, part8, once, tb, ub, slot, arcs, nlse2, alpha, beta, dz, de, dp;
 };
 
 void loss_plan(LossPlan &p) {
@@ -123,6 +125,7 @@ void loss_plan(LossPlan &p) {
   p.w = loss_pick(p.pd, p.V1, p.H, (m + 31) / 32, true);
   p.parts = 2 * ((p.V1 + p.x.bn - 1) / p.x.bn);
   p.narrow = loss_narrow((p.pd == 3 ? kLossShapesF32 : kLossShapes)[p.x.shape], p.V1);
+  p.fold_once = p.kind == kLossLattice && N * p.hd * 4 >= kLatticeOnce;
   p.sort = p.kind == kLossDistill && p.K > 2 && p.K <= kLossSortMost && N * p.K > kLossSmall && (double)N * p.K * p.parts >= kLossSortWork;
   p.join = !p.narrow && !p.sort && N * p.K <= kLossJoinEntries && p.parts <= kLossJoinParts;
   p.dw_direct = p.chunks == 1 && p.w.splits == 1;
@@ -158,6 +161,7 @@ void loss_plan(LossPlan &p) {
     p.tb = take((size_t)p.B * 4);
     p.ub = take((size_t)p.B * 4);
     p.place = take((size_t)p.B * 4);
+    p.part8 = take((size_t)p.B * 4);
     p.slot = take(R * 4);
     p.arcs = take((size_t)p.places * 16);
     p.nlse2 = take(n * 4);
@@ -168,6 +172,7 @@ void loss_plan(LossPlan &p) {
     p.dw = p.dw_direct ? at : take((size_t)p.w.splits * p.V1 * p.hd * 4);
     p.dz = p.dz_direct ? at : take((size_t)p.z.splits * R * p.hd * 4);
     if (p.kind == kLossLattice) {
+      if (p.fold_once) p.once = take((R / kFoldFrames + (size_t)(p.B + 2) * (p.U + 1)) * p.hd * 4);
       p.alpha = take((size_t)p.places * 8);
       p.beta = take((size_t)p.places * 8);
       if (p.chunks > 1) {
@@ -563,6 +568,7 @@ int wind_transducer_loss(const wind_output_layer *layer, const void *e, int64_t 
   l.count = r.at<int>(p.count);
   l.nodes = LossNodes{r.at<float4>(p.arcs), r.at<int>(p.slot), r.at<float>(p.nlse2)};
   l.place = r.at<int>(p.place);
+  l.part = r.at<int>(p.part8);
   l.cells = p.cells;
   l.skew = p.skew;
   if (p.grads) {
@@ -609,6 +615,12 @@ int wind_transducer_loss(const wind_output_layer *layer, const void *e, int64_t 
       if (c > 0) rows_of_chunk(c);
       lattice_counts_kernel<<<p.R / 256, 256, 0, s>>>(l, r.chunk);
       const LossFinish f = loss_gradients(r, c, n_e + n_p > 0, LossOut{}, dw, db);
+      if (p.fold_once && n_e && n_p) {
+        const LatticeOnce once{r.at<float>(p.once), B * ((T + kFoldFrames - 1) / kFoldFrames) * (int)over};
+        lattice_finish_once_kernel<<<(unsigned)(f.n_db + f.n_dw + once.n), 256, 0, s>>>(f, r.chunk, l, fold, once);
+        lattice_parts_kernel<<<dim3((unsigned)B * (unsigned)(U + 1), (unsigned)over), 256, 0, s>>>(l, r.chunk, fold, once);
+        continue;
+      }
       const int blocks = f.n_db + f.n_dw + n_e + n_p;
       if (blocks) lattice_finish_kernel<<<(unsigned)blocks, 256, 0, s>>>(f, r.chunk, l, fold, n_e);
     }

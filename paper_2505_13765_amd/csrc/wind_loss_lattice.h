@@ -23,11 +23,12 @@ struct LatticeDev {
   const int *labels, *frames, *counts;        // [B, U], [B], [B]
   const float *weights;                       // [B] or null
   float *loss;                                // [B]
-  int *tb, *ub, *off, *place, *count;         // frames (0: left out) and labels as they are used, first row, first place, rows in all
+  int *tb, *ub, *off, *place, *part, *count;  // frames (0: left out) and labels as they are used, first row, place and part of dp, rows in all
   int cells, skew;                            // cells of a thread; 1: places lie diagonal by diagonal
   LossNodes nodes;
   float2 *alpha, *beta;                       // per place: mantissa, exponent (int bits)
 };
+constexpr int kFoldFrames = 8;         // frames whose dz a workgroup folds at a time
 // places of T frames of U1 nodes; that of node (0, u), from which those of the later frames follow U1 apart
 __device__ __forceinline__ int lattice_places(const LatticeDev &l, int T, int U1) { return T ? (T + (l.skew ? (U1 - 1) / l.cells : 0)) * U1 : 0; }
 __device__ __forceinline__ int lattice_place(const LatticeDev &l, int first, int U1, int u) { return first + u + (l.skew ? u / l.cells * U1 : 0); }
@@ -36,7 +37,7 @@ __device__ __forceinline__ const char *lattice_p(const LatticeDev &l, int b, int
 
 // One workgroup: which utterances count, and where their rows begin; returns the number of rows.
 __device__ __forceinline__ int lattice_rows(const LatticeDev &l) {
-  __shared__ int wave_sum_[2][4], total_[2];
+  __shared__ int wave_sum_[3][4], total_[3];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   // the lanes of a group look through an utterance's labels
   int group = 1;
@@ -64,17 +65,18 @@ __device__ __forceinline__ int lattice_rows(const LatticeDev &l) {
     }
   }
   __syncthreads();
-  if (tid < 2) total_[tid] = 0;
+  if (tid < 3) total_[tid] = 0;
   __syncthreads();
   for (int base = 0; base < l.B; base += 256) {
     const int b = base + tid;
-    int n[2] = {0, 0}, sum[2], at[2];
+    int n[3] = {0, 0, 0}, sum[3], at[3];
     if (b < l.B) {
       n[0] = l.tb[b] * (l.ub[b] + 1);
       n[1] = lattice_places(l, l.tb[b], l.ub[b] + 1);
+      n[2] = (l.tb[b] + kFoldFrames - 1) / kFoldFrames * (l.ub[b] + 1);
     }
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
+    for (int q = 0; q < 3; ++q) {
       sum[q] = n[q];
       for (int d = 1; d < 64; d <<= 1) {
         const int o = __shfl_up(sum[q], d);
@@ -84,15 +86,16 @@ __device__ __forceinline__ int lattice_rows(const LatticeDev &l) {
     }
     __syncthreads();
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
+    for (int q = 0; q < 3; ++q) {
       at[q] = total_[q];
       for (int w = 0; w < wave; ++w) at[q] += wave_sum_[q][w];
-      if (b < l.B) (q ? l.place : l.off)[b] = at[q] + sum[q] - n[q];
+      if (b < l.B) (q == 0 ? l.off : q == 1 ? l.place : l.part)[b] = at[q] + sum[q] - n[q];
     }
     __syncthreads();
     if (tid == 255) {
       total_[0] = at[0] + sum[0];
       total_[1] = at[1] + sum[1];
+      total_[2] = at[2] + sum[2];
     }
     __syncthreads();
   }
@@ -397,6 +400,106 @@ __device__ __forceinline__ void lattice_fold(const LatticeDev &l, const LossChun
   f32x4 *o = reinterpret_cast<f32x4 *>(f.sum[which] + (size_t)row * f.ld + c);
   *o = j0 > 0 ? *o + s : s;
 }
+// Both folds in one reading of dz, for large lattices: a workgroup takes 8 frames of an utterance and 256 columns, its waves every fourth u.  A frame's sum
+// over u is done with that; a prediction row's is of 8 frames and goes to a part of dp, an eighth of dz, which lattice_parts_kernel adds up.  (165000 nodes
+// of 640: 150 us for the folds apart, 90 so.)
+struct LatticeOnce {
+  float *parts;                // per utterance that the chunk meets [frames / 8][U1][ld]
+  int n;                       // workgroups (0: the folds apart)
+};
+// the chunk's first part, as an utterance's parts are numbered
+__device__ __forceinline__ int lattice_first_part(const LatticeDev &l, int c0) {
+  const LatticeNode d = lattice_node(l, c0);
+  return l.part[d.b] + d.t / kFoldFrames * d.U1;
+}
+__device__ __forceinline__ void lattice_fold_once(const LatticeDev &l, const LossChunk &k, const LatticeFold &f, const LatticeOnce &o, int block) {
+  __shared__ f32x4 sums[4][kFoldFrames][64];
+  const int across = (f.ld + 255) / 256, row = block / across, blocks = (l.T + kFoldFrames - 1) / kFoldFrames;
+  const int b = row / blocks, t0 = (row - b * blocks) * kFoldFrames, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (block - row * across) * 256 + lane * 4;
+  const int live = chunk_rows(k), T = l.tb[b], U1 = l.ub[b] + 1, first = l.off[b] + t0 * U1;
+  const bool whole = f.sum[0] == nullptr;
+  const int frames = min(kFoldFrames, T - t0);                // of the utterance
+  if (whole)
+    for (int i = wave; i < min(kFoldFrames, l.T - t0); i += 4)
+      if (i >= frames && c < l.H) lattice_store4(l, f.out[0], (size_t)b * l.T + t0 + i, c, f32x4{0.f, 0.f, 0.f, 0.f});
+  if (frames <= 0 || first >= k.c0 + live || first + frames * U1 <= k.c0) return;
+  f32x4 e[kFoldFrames], de[kFoldFrames];
+#pragma unroll
+  for (int i = 0; i < kFoldFrames; ++i) {
+    de[i] = e[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (i < frames && c < l.H) e[i] = lattice_load4(l, lattice_e(l, b, t0 + i), c);
+  }
+  float *const parts = o.parts + (size_t)(l.part[b] + t0 / kFoldFrames * U1 - lattice_first_part(l, k.c0)) * f.ld + c;
+  if (c < l.H)
+    for (int u = wave; u < U1; u += 4) {
+      f32x4 v[kFoldFrames], s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < kFoldFrames; ++i) {
+        const int n = first + i * U1 + u - k.c0;
+        v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (i < frames && n >= 0 && n < live) {
+          const float *at = f.dz + (size_t)n * f.ld + c;
+          v[i] = *reinterpret_cast<const f32x4 *>(at);
+          for (int q = 1; q < f.splits; ++q) v[i] += *reinterpret_cast<const f32x4 *>(at + (size_t)q * f.part);
+        }
+      }
+      const f32x4 p = lattice_load4(l, lattice_p(l, b, u), c);
+#pragma unroll
+      for (int i = 0; i < kFoldFrames; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float x = e[i][j] + p[j] > 0.f ? v[i][j] : 0.f;
+          de[i][j] += x;
+          s[j] += x;
+        }
+      *reinterpret_cast<f32x4 *>(parts + (size_t)u * f.ld) = s;
+    }
+#pragma unroll
+  for (int i = 0; i < kFoldFrames; ++i) sums[wave][i][lane] = de[i];
+  __syncthreads();
+  for (int i = wave; i < frames; i += 4) {
+    const int n = first + i * U1;                             // the frame's first row
+    if (c >= l.H || n >= k.c0 + live || n + U1 <= k.c0) continue;
+    const f32x4 s = (sums[0][i][lane] + sums[1][i][lane]) + (sums[2][i][lane] + sums[3][i][lane]);
+    const size_t to = (size_t)b * l.T + t0 + i;
+    if (whole) lattice_store4(l, f.out[0], to, c, s);
+    else {
+      f32x4 *at = reinterpret_cast<f32x4 *>(f.sum[0] + to * f.ld + c);
+      *at = n < k.c0 ? *at + s : s;
+    }
+  }
+}
+// A prediction row's parts of the chunk: a workgroup one row and 256 columns.
+__global__ __launch_bounds__(256) void lattice_parts_kernel(LatticeDev l, LossChunk k, LatticeFold f, LatticeOnce o) {
+  __shared__ f32x4 sums[4][64];
+  const int live = chunk_rows(k), row = blockIdx.x, b = row / (l.U + 1), u = row - b * (l.U + 1);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (int)blockIdx.y * 256 + lane * 4;
+  const int T = l.tb[b], U1 = l.ub[b] + 1, first = l.off[b];
+  const bool whole = f.sum[1] == nullptr;
+  if (T == 0 || u >= U1) {
+    if (whole && wave == 0 && c < l.H) lattice_store4(l, f.out[1], row, c, f32x4{0.f, 0.f, 0.f, 0.f});
+    return;
+  }
+  if (first + u >= k.c0 + live || first + T * U1 <= k.c0) return;
+  // blocks of 8 frames that the chunk meets
+  const int step = kFoldFrames * U1, x0 = max(0, k.c0 - first) / step, x1 = min((T + kFoldFrames - 1) / kFoldFrames, (k.c0 + live - first + step - 1) / step);
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  if (c < l.H) {
+    const int base = l.part[b] - lattice_first_part(l, k.c0) + u;   // (+ x U1: not below zero from x0 on)
+#pragma unroll 4
+    for (int x = x0 + wave; x < x1; x += 4) s += *reinterpret_cast<const f32x4 *>(o.parts + (size_t)(base + x * U1) * f.ld + c);
+  }
+  sums[wave][lane] = s;
+  __syncthreads();
+  if (wave || c >= l.H) return;
+  s = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+  if (whole) {
+    lattice_store4(l, f.out[1], row, c, s);
+    return;
+  }
+  f32x4 *to = reinterpret_cast<f32x4 *>(f.sum[1] + (size_t)row * f.ld + c);
+  *to = first + u < k.c0 ? *to + s : s;
+}
 // The last launch of a chunk: db, the sums over parts of dW, and what dz gives to encoder and prediction rows.
 __global__ __launch_bounds__(256) void lattice_finish_kernel(LossFinish f, LossChunk k, LatticeDev l, LatticeFold fold, int n_e) {
   int block = (int)blockIdx.x;
@@ -405,6 +508,12 @@ __global__ __launch_bounds__(256) void lattice_finish_kernel(LossFinish f, LossC
   if (which) block -= n_e;
   if (fold.wide[which] == 256) lattice_fold<256>(l, k, fold, which, block);
   else lattice_fold<64>(l, k, fold, which, block);
+}
+
+// The same of a large lattice.
+__global__ __launch_bounds__(256) void lattice_finish_once_kernel(LossFinish f, LossChunk k, LatticeDev l, LatticeFold fold, LatticeOnce o) {
+  int block = (int)blockIdx.x;
+  if (!loss_finish(f, k, block)) lattice_fold_once(l, k, fold, o, block);
 }
 
 // The sums of several chunks, rounded once; rows that no utterance has are zero.

@@ -267,6 +267,16 @@ def test_lattice_in_chunks():
     check(wind.transducer_loss(*a, grad=GRAD), transducer_loss(*a), GRAD)
 
 
+def test_a_large_lattice_in_one_chunk():
+    wind = api()
+    a = lattice(3, 203, 40, 701, 40, "bf16", 16)
+    a[0], a[1] = torch.nan_to_num(a[0]), torch.nan_to_num(a[1], posinf=0.0)
+    a[4] = a[4].clamp(min=0)
+    a[5][1] = 0
+    check(wind.transducer_loss(*a, grad=GRAD), transducer_loss(*a), GRAD)
+    check(wind.transducer_loss(*a, grad=("e",)), transducer_loss(*a), ("e",))
+
+
 def test_gradients_against_differences():
     """Along a random direction of every input, fp32.  A central difference over 2 s is off by the losses' own bounds over s, and by its truncation,
     which is that of the same difference of the reference."""
