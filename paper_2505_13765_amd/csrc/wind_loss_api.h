@@ -4,13 +4,12 @@
 
 namespace {
 
-// Tiles of the products.  rate: of a full chip of them, in parts of kLossRate, for logits and for the products of dx; alone: the part of that left when a CU has one workgroup of them
-// instead of two; start: a tile's start and results, in slabs.  256 x 128 outputs in two workgroups per CU against 256 x 256 in one, sums over 640: 34 us instead of 50 for 5700 rows
-// and 4097 outputs (one's start and results behind the other's products), 1 to 5 % less over 2048; the products of dx, whose sums are
-// longer and whose results cost less: 1.51 ms in one workgroup of 256 x 256, 1.86 in two of 256 x 128 (7373 x 2048 over 65537).
-struct LossShape { int bm, bn; double rate, rate_dx, alone, start; };
-constexpr LossShape kLossShapes[] = {{256, 256, 0.9, 1.15, 1.0, 12}, {256, 128, 1.0, 1.0, 0.65, 6}, {128, 128, 0.87, 0.87, 0.55, 6}, {64, 64, 0.35, 0.35, 1.0, 8}};
-constexpr LossShape kLossShapesF32[] = {{128, 128, 0.75, 0.75, 1.0, 12}, {64, 64, 0.6, 0.6, 0.65, 8}};
+// Tiles of the logits.  rate: of a full chip of them, in parts of kLossRate; alone: the part of that left when a CU has one workgroup of them instead of
+// two; start: a tile's start and results, in slabs.  256 x 128 outputs in two workgroups per CU against 256 x 256 in one, sums over 640: 34 us instead
+// of 50 for 5700 rows and 4097 outputs (one's start and results behind the other's products), 1 to 5 % less over 2048.
+struct LossShape { int bm, bn; double rate, alone, start; };
+constexpr LossShape kLossShapes[] = {{256, 256, 0.9, 1.0, 12}, {256, 128, 1.0, 0.65, 6}, {128, 128, 0.87, 0.55, 6}, {64, 64, 0.35, 1.0, 8}};
+constexpr LossShape kLossShapesF32[] = {{128, 128, 0.75, 1.0, 12}, {64, 64, 0.6, 0.65, 8}};
 constexpr double kLossRate = 1.2e15 / 256 / 1e6;   // operations per microsecond and CU
 // the tile of each shape for operands of PA and PB planes
 template <int PA, int PB>
@@ -41,11 +40,11 @@ constexpr size_t kLossChunkBytes = 1200u << 20;
 constexpr int kLossMaxEntries = 1024;
 // Entries (of all rows) and column blocks up to which a row tile's last workgroup joins its column blocks: one launch less, 36 -> 31 us for 16 rows of 1025
 // outputs.  With more, that workgroup is what the others' results wait for (3001 rows of 64 entries: 73 us against 51 and 6).
+constexpr long long kLossJoinEntries = 4096;
+constexpr int kLossJoinParts = 128;
 // Entries x column blocks from which entries are sorted by column block: a launch of 6 to 8 us against every tile looking at all of its rows' entries (12000 rows,
 // 16 entries, 130 blocks: 838 -> 788 us a step; 3476, 23, 112, fp32 losses: 143 -> 137; 3001, 64, 18: even).
 constexpr double kLossSortWork = 4e6;
-constexpr long long kLossJoinEntries = 4096;
-constexpr int kLossJoinParts = 128;
 // Sums of dz that 16 threads share instead of 4: of at least kLatticeLong rows, where 4 would leave the chip short of workgroups (240 frames of 2 labels, 24
 // utterances: 56 us for 96 of them; with thousands, 750 frames of 121, 16 threads cost 6 % of the whole step).
 constexpr int kLatticeLong = 64;
@@ -62,9 +61,9 @@ int lattice_planes(int dtype) { return dtype == WIND_BF16 ? 2 : 3; }
 bool loss_narrow(const LossShape &s, long long n) { return s.bn >= 128 && n % s.bn > 0 && n % s.bn <= 64 && n / s.bn <= 16; }
 
 struct LossPick { int shape, splits, bm, bn; };
-// Shape, and parts of the summed axis, of a product of m x n outputs over `slabs` slabs of 32: the least time of the fullest CU, where a tile costs
-// its operations, its start and its results, and parts cost the writing and reading of their sums.
-LossPick loss_pick(int planes, long long m, long long n, long long slabs, bool split) {
+// Shape of the logits' tiles, m x n outputs over `slabs` slabs of 32: the least time of the fullest CU, where a tile costs its operations, its start
+// and its results.
+LossPick loss_pick(int planes, long long m, long long n, long long slabs) {
   const LossShape *shapes = planes == 3 ? kLossShapesF32 : kLossShapes;
   const int count = planes == 3 ? 2 : 4, products = planes == 3 ? 6 : planes;
   LossPick best{0, 1, 0, 0};
@@ -72,19 +71,75 @@ LossPick loss_pick(int planes, long long m, long long n, long long slabs, bool s
   for (int t = 0; t < count; ++t) {
     const LossShape &s = shapes[t];
     const long long tiles = ((m + s.bm - 1) / s.bm) * ((n + s.bn - 1) / s.bn);
-    const double weight = loss_narrow(s, n) && !split ? tiles - 0.55 * ((m + s.bm - 1) / s.bm) : (double)tiles;
-    for (int parts = 1; parts <= (split ? 64 : 1); ++parts) {
-      if (parts > 1 && (slabs / parts < 8 || tiles * parts > 1024)) break;
-      const double fullest = std::ceil(weight * parts / 256);
-      const double tile = ((double)((slabs + parts - 1) / parts) * products + s.start) * s.bm * s.bn * 64 / (kLossRate * (split ? s.rate_dx : s.rate) * (fullest == 1 ? s.alone : 1.0));
-      const double time = fullest * tile + (parts > 1 ? 1.0 + parts * (double)m * n * 8 / 4e6 : 0.0);
-      if (time < least) {
-        least = time;
-        best = LossPick{t, parts, s.bm, s.bn};
-      }
+    const double fullest = std::ceil((loss_narrow(s, n) ? tiles - 0.55 * ((m + s.bm - 1) / s.bm) : (double)tiles) / 256);
+    const double time = fullest * ((double)slabs * products + s.start) * s.bm * s.bn * 64 / (kLossRate * s.rate * (fullest == 1 ? s.alone : 1.0));
+    if (time < least) {
+      least = time;
+      best = LossPick{t, 1, s.bm, s.bn};
     }
   }
   return best;
+}
+
+// Tiles of the products of dx: dz (rows x H over outputs) and dW (outputs x H over rows) go in one launch on tiles of one shape, dz first, where dW's
+// tiles fill what dz's leave free.  rate: operations per microsecond of a CU with `pair` workgroups; alone: a workgroup's own rate on a CU of its own
+// against the two; start: as above; chip: operations per microsecond of the whole chip, whose clock falls with its load.  From the times of 70 problems (1
+// to 180000 rows, 33 to 65537 outputs, 50 to 2048 units) on each shape with 1 to 64 parts: what this picks takes 1 % more than the best of each,
+// shapes picked for each product by itself took 4 %.  10000 rows of 8193 outputs over 1024: 752 -> 692 us a step, 2000 of 5615 over 147: 267 -> 216.
+struct ProductShape { int bm, bn, pair; double rate, alone, start, chip; };
+constexpr ProductShape kProductShapes[] = {
+    {256, 256, 1, 7.0e6, 1.0, 12, 3.2e9}, {256, 128, 2, 8.7e6, 0.73, 10, 1.53e9}, {128, 128, 2, 8.2e6, 0.81, 12, 1.17e9}, {64, 64, 1, 2.2e6, 1.0, 10, 1.6e9}};
+constexpr ProductShape kProductShapesF32[] = {{128, 128, 1, 7.6e6, 1.0, 37, 1.64e9}, {64, 64, 2, 6.5e6, 0.56, 18, 1.1e9}};
+constexpr int kProductParts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+
+// when `slots` workgroups at a time end that take nz tiles of time a each, then nw of time b
+double products_end(long long nz, double a, long long nw, double b, long long slots) {
+  const long long late = nz % slots;                               // slots with one tile of dz more
+  const double lo = (double)(nz / slots) * a, hi = late ? lo + a : lo;
+  const double even = ((double)nw * b + lo * (double)(slots - late) + hi * (double)late) / (double)slots;
+  double end = even + b;
+  for (const double from : {lo, hi}) {                             // the least end, a whole number of dW's tiles behind lo or hi, by which nw are done
+    const double k = std::max(0.0, std::floor((even - from) / b));
+    for (int i = 0; i < 2; ++i) {
+      const double t = from + (k + i) * b;
+      const double done = (double)late * std::max(0.0, std::floor((t - hi) / b + 1e-6)) + (double)(slots - late) * std::max(0.0, std::floor((t - lo) / b + 1e-6));
+      if (done >= (double)nw) end = std::min(end, t);
+    }
+  }
+  return std::max(end, hi);
+}
+void products_pick(int planes, long long m, long long V1, long long H, LossPick &z, LossPick &w) {
+  const ProductShape *shapes = planes == 3 ? kProductShapesF32 : kProductShapes;
+  const int count = planes == 3 ? 2 : 4, products = planes == 3 ? 6 : 1;
+  const long long z_slabs = (V1 + 31) / 32, w_slabs = (m + 31) / 32;
+  // parts: what their sums cost to write and read
+  const double once = planes == 3 ? 1.7 : 2.8, rate = planes == 3 ? 3.6e6 : 4.5e6;
+  auto join = [&](int parts, long long rows) { return parts > 1 ? once + parts * (double)rows * (double)H * 8 / rate : 0.0; };
+  double least = 1e300;
+  for (int t = 0; t < count; ++t) {
+    const ProductShape &s = shapes[t];
+    const long long across = (H + s.bn - 1) / s.bn, z_tiles = (m + s.bm - 1) / s.bm * across, w_tiles = (V1 + s.bm - 1) / s.bm * across;
+    const double slab = (double)s.bm * s.bn * 64 / s.rate, chip = 4.0 * (double)m * (double)H * (double)V1 * products / s.chip;
+    const long long most = 1024 * s.pair;
+    for (const int pz : kProductParts) {
+      if (pz > 1 && (z_slabs / pz < 8 || z_tiles * pz > most)) break;
+      const double a = ((double)((z_slabs + pz - 1) / pz) * products + s.start) * slab, z_join = join(pz, m);
+      for (const int pw : kProductParts) {
+        if (pw > 1 && (w_slabs / pw < 8 || w_tiles * pw > most)) break;
+        const double b = ((double)((w_slabs + pw - 1) / pw) * products + s.start) * slab;
+        const long long nz = z_tiles * pz, nw = w_tiles * pw;
+        double time = s.pair == 1      ? products_end(nz, a, nw, b, 256)
+                      : nz + nw <= 256 ? std::max(a, b) / s.alone
+                                       : products_end(nz, 2 * a, nw, 2 * b, 512);
+        time = std::max(time, chip) + 0.1 * std::min(time, chip) + z_join + join(pw, V1);   // (a chip at its own limit still wants its CUs busy to the end)
+        if (time < least) {
+          least = time;
+          z = LossPick{t, pz, s.bm, s.bn};
+          w = LossPick{t, pw, s.bm, s.bn};
+        }
+      }
+    }
+  }
 }
 
 struct LossPlan {
@@ -120,9 +175,10 @@ void loss_plan(LossPlan &p) {
   p.R = (int)round_up((size_t)((N + p.chunks - 1) / p.chunks), 256);
   p.chunks = (int)((N + p.R - 1) / p.R);
   const long long m = std::min<long long>(p.R, N);
-  p.x = loss_pick(p.pa, m, p.V1, p.hblk, false);
-  p.z = loss_pick(p.pd, m, p.H, p.vblk, true);
-  p.w = loss_pick(p.pd, p.V1, p.H, (m + 31) / 32, true);
+  p.x = loss_pick(p.pa, m, p.V1, p.hblk);
+  // (of the cells of a padded batch about two thirds count, where its utterances' lengths lie between half of the longest and the whole; chunks but
+  // the last are full of cells that count)
+  if (p.grads) products_pick(p.pd, p.kind == kLossLattice && p.B > 1 && p.chunks == 1 ? std::max(m * 2 / 3, 1ll) : m, p.V1, p.H, p.z, p.w);
   p.parts = 2 * ((p.V1 + p.x.bn - 1) / p.x.bn);
   p.narrow = loss_narrow((p.pd == 3 ? kLossShapesF32 : kLossShapes)[p.x.shape], p.V1);
   p.fold_once = p.kind == kLossLattice && N * p.hd * 4 >= kLatticeOnce;
@@ -337,15 +393,12 @@ LossFinish loss_gradients(const LossRun &r, int chunk, bool dz, LossOut dz_out, 
     }
   }
   const LossProduct z{dx, r.w, p.vblk, p.H, (p.H + p.z.bn - 1) / p.z.bn}, w{dx, r.x, 0, p.V1, (p.H + p.w.bn - 1) / p.w.bn};
-  const unsigned z_blocks = loss_grid((p.R + p.z.bm - 1) / p.z.bm, z.ct, zo.splits), w_blocks = loss_grid((p.V1 + p.w.bm - 1) / p.w.bm, w.ct, wo.splits);
-  if (dz && dw && p.z.shape == p.w.shape) {
+  const unsigned z_blocks = dz ? loss_grid((p.R + p.z.bm - 1) / p.z.bm, z.ct, zo.splits) : 0;
+  const unsigned w_blocks = dw ? loss_grid((p.V1 + p.w.bm - 1) / p.w.bm, w.ct, wo.splits) : 0;
+  if (dz || dw)
     loss_with_dx_tile(p.pd, p.z.shape, [&](auto t) {
       loss_products_kernel<decltype(t)><<<z_blocks + w_blocks, 256, 0, r.s>>>(z, zo, (int)z_blocks, w, wo, r.chunk);
     });
-    return f;
-  }
-  if (dz) loss_with_dx_tile(p.pd, p.z.shape, [&](auto t) { loss_dz_kernel<decltype(t)><<<z_blocks, 256, 0, r.s>>>(z, r.chunk, zo); });
-  if (dw) loss_with_dx_tile(p.pd, p.w.shape, [&](auto t) { loss_dw_kernel<decltype(t)><<<w_blocks, 256, 0, r.s>>>(w, r.chunk, wo); });
   return f;
 }
 

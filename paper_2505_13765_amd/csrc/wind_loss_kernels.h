@@ -908,22 +908,8 @@ __device__ __forceinline__ void loss_product(int bid, const LossProduct &g, cons
   else loss_clear<T>(acc);
   loss_store<T>(o, acc, ti * T::BM, rows, tj * T::BN, split, smem);
 }
-// dz = dx W: rows of the chunk against columns of W's panels, summed over outputs.
-template <class T>
-__global__ __launch_bounds__(256, T::W) void loss_dz_kernel(LossProduct g, LossChunk k, LossOut o) {
-  __shared__ __attribute__((aligned(256))) unsigned char smem[T::SMEM];
-  loss_product<T, false, true>((int)blockIdx.x, g, o, chunk_rows(k), g.slabs, smem);
-}
-// dW = dx^T z: columns of dx's panels against columns of z's, summed over the chunk's rows.
-template <class T>
-__global__ __launch_bounds__(256, T::W) void loss_dw_kernel(LossProduct g, LossChunk k, LossOut o) {
-  __shared__ __attribute__((aligned(256))) unsigned char smem[T::SMEM];
-  const int live = chunk_rows(k);
-  if (o.add && live == 0) return;
-  loss_product<T, true, true>((int)blockIdx.x, g, o, g.cols, (live + 31) / 32, smem);
-}
-
-// Both in one launch, on tiles of one shape.
+// dz = dx W: rows of the chunk against columns of W's panels, summed over outputs.  dW = dx^T z: columns of dx's panels against columns of z's, summed over
+// the chunk's rows.  In one launch, on tiles of one shape.
 template <class T>
 __global__ __launch_bounds__(256, T::W) void loss_products_kernel(LossProduct z, LossOut zo, int z_blocks, LossProduct w, LossOut wo, LossChunk k) {
   __shared__ __attribute__((aligned(256))) unsigned char smem[T::SMEM];
