@@ -118,6 +118,10 @@ __device__ __forceinline__ void loss_mainloop(const PanelsDev &a, const PanelsDe
     fetched();
   }
   init();
+  // Of six products the five smaller ones have sums of their own: added to the large one they would round it six times a K step instead of once
+  // (1952 hidden units: db of a lattice off by 4e-6 relative).
+  constexpr bool SIX = T::PAIRS == 6;
+  f32x16 low[SIX ? T::MI : 1][SIX ? T::NI : 1] = {};
 
   bf16x8 af[2][T::PA][T::MI], bfr[2][T::PB][T::NI];
   const int frow = lane & 31, half = lane >> 5;
@@ -152,7 +156,8 @@ __device__ __forceinline__ void loss_mainloop(const PanelsDev &a, const PanelsDe
       // planes of the pair, the smallest product first: (2, 0) (0, 2) (1, 1) (1, 0) (0, 1) (0, 0), or (1, 0) (0, 0)
       const int pa = T::PAIRS == 6 ? (pair == 0 ? 2 : pair == 2 || pair == 3 ? 1 : 0) : T::PA - 1 - pair;
       const int pb = T::PAIRS == 6 ? (pair == 1 ? 2 : pair == 2 || pair == 4 ? 1 : 0) : 0;
-      acc[mi][ni] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bfr[set][pb][ni], af[set][pa][mi], acc[mi][ni], 0, 0, 0);
+      f32x16 &to = SIX && pair < 5 ? low[SIX ? mi : 0][SIX ? ni : 0] : acc[mi][ni];
+      to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bfr[set][pb][ni], af[set][pa][mi], to, 0, 0, 0);
       if (reads) {
 #pragma unroll
         for (int y = 0; y < PER; ++y)
@@ -191,6 +196,10 @@ __device__ __forceinline__ void loss_mainloop(const PanelsDev &a, const PanelsDe
 #pragma unroll
   for (int step = 0; step + 1 < STEPS; ++step) kstep(step & 1, true, slot, step + 1, none);
   kstep(1, false, slot, 0, none);
+  if (SIX) {
+#pragma unroll
+    for (int x = 0; x < T::MI * T::NI; ++x) acc[x / T::NI][x % T::NI] += low[SIX ? x / T::NI : 0][SIX ? x % T::NI : 0];
+  }
   wait_vmcnt<0>();
   __syncthreads();
 }
