@@ -421,3 +421,26 @@ def test_a_training_step_of_a_joiner():
     assert len(tokens) == 2
     model.close()
     teacher.close()
+
+
+@pytest.mark.parametrize("N", (1, 13, 128))
+def test_gradients_of_few_rows_are_only_rounded_once(N):
+    """bf16 gradients of few rows: off by the result's own rounding (half a step, 2^-8 relative) and what dx on 16 bits leaves, not by a rounding of dx to 8 bits.
+
+    dx_v = c (p_v - [v = label]) is kept to 2^-16 of itself, p_v to its logit's error, at most (H + 2) 2^-24 sum |h w| with the bias (one rounding a term) and twice that for
+    the norm's, and 2^-20 for the functions and sums; products add (terms + 8) 2^-24 of their terms' sum.  The weight 1 + 2^-8 lies between two bf16 values: rounded to 8 bits, the
+    label's dx alone, which is almost all of the gradient, would be off by 2^-8."""
+    wind, H, V1 = api(), 64, 400
+    g = torch.Generator().manual_seed(N)
+    h, w = (0.25 * torch.randn(s, H, generator=g) for s in (N, V1))
+    b, labels = 0.1 * torch.randn(V1, generator=g), torch.randint(0, V1, (N,), generator=g, dtype=torch.int32)
+    h, w, c = h.bfloat16(), w.bfloat16(), 1 + 2.0**-8
+    _, dh, dw = wind.label_loss(h.cuda(), w.cuda(), b.cuda(), labels.cuda(), weights=torch.full((N,), c).cuda(), grad=("h", "w"))
+    h, w, b = h.double(), w.double(), b.double()
+    p = torch.softmax(h @ w.T + b, dim=1)
+    dx = c * (p - torch.nn.functional.one_hot(labels.long(), V1))
+    logit = 2 * (H + 2) * 2.0**-24 * (h.abs() @ w.abs().T + b.abs()).amax(1, keepdim=True) + 2.0**-20
+    off = 2.0**-16 * dx.abs() + c * p * logit
+    for got, ref, bound in ((dh, dx @ w, off @ w.abs() + (V1 + 8) * 2.0**-24 * (dx.abs() @ w.abs())), (dw, dx.T @ h, off.T @ h.abs() + (N + 8) * 2.0**-24 * (dx.abs().T @ h.abs()))):
+        err = (got.double().cpu() - ref).abs()
+        assert (err <= 2.0**-8 * (ref.abs() + bound) + bound + 2.0**-133).all(), (err - 2.0**-8 * ref.abs()).max()
