@@ -413,7 +413,8 @@ int wind_transducer_loss_workspace_bytes(const wind_output_layer *layer, int B, 
  *   labels      DEVICE [B, U] int32, 0 .. V1 - 2
  *   frames, label_counts   DEVICE [B] int32, clamped to 0 .. T and 0 .. U.  What lies beyond them is not looked at.  An utterance without
  *               frames is left out (loss 0, no gradient); one with a label that does not exist is left out and its loss is NaN; one of probability zero
- *               has loss +inf and no gradient
+ *               has loss +inf and no gradient.  (Probabilities are kept down to 2^-268000000 or so, losses of 186 million; a path below that, as
+ *               through an output that b masks with -1e9, counts as impossible)
  *   loss        DEVICE [B] fp32;  de [B, T, H], dp [B, U + 1, H] (zeros beyond frames and label_counts), dw [V1, H], db [V1]
  * U <= 4095, T * (U + 1) < 2^27, B * T * (U + 1) < 2^31 and B * (T + U + 1) * H / 64 < 2^31 (WIND_ERR_UNSUPPORTED).
  */

@@ -520,9 +520,9 @@ __device__ __forceinline__ void loss_bias(const float *bias, int cols, int col0,
 // A probability as mantissa and exponent, m 2^e (wind_loss_lattice.h); zero has an exponent below every other's.
 struct Cell { float m; int e; };
 constexpr int kCellZero = -(1 << 28);
-__device__ __forceinline__ Cell cell_of_log2(float l) {   // 2^l, 1 <= m < 2
-  if (l == -__builtin_inff()) return Cell{0.f, kCellZero};
-  const float f = floorf(l);
+// 2^l, 1 <= m < 2.  Below 2^kCellZero (an output masked by -1e30, say) it is zero: sums of three exponents that began lower would leave the integers' range.
+__device__ __forceinline__ Cell cell_of_log2(float l) {
+  const float f = fmaxf(floorf(l), (float)kCellZero);
   return Cell{__builtin_amdgcn_exp2f(l - f), (int)f};
 }
 struct LossNodes {

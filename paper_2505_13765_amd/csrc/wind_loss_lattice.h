@@ -8,7 +8,8 @@
 // in another order where there are at least as many frames as labels: diagonal by diagonal of the threads that run them, so that what a wave asks for
 // at a time is consecutive memory (by rows, 64 lanes touch 64 cache lines).
 //
-// Numbers.  A cell is a mantissa and an exponent of its own (m 2^e, 0.5 <= m < 1, e a 32-bit integer).  A step of the recursion is then two
+// Numbers.  A cell is a mantissa and an exponent of its own (m 2^e, 0.5 <= m < 1, an arc's 1 <= m < 2, e a 32-bit integer of -2^28 or more: what is
+// below 2^-2^28 counts as zero).  A step of the recursion is then two
 // products and one addition in fp32, relative error 2^-23 per step however improbable the cell, and no logarithm or exponential on
 // the chain.  Logarithms of probabilities in fp32 lose 2^-24 of their size at every step, at -2000 a ten-thousandth of the probability.
 #pragma once
