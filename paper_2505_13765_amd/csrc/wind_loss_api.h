@@ -163,8 +163,8 @@ struct LossPlan {
   bool sort;                         // entries sorted by column block
   bool join;                         // joined by the launch that makes them
   // offsets into the workspace
-  size_t idx, state, count, ticket, wp, rows, label, value, coef, scale, lse2, logit, part, sorted, begin, dx, colsum, dw, total;
-  size_t off, place, part8, once, tb, ub, slot, arcs, nlse2, alpha, beta, dz, de, dp;
+  size_t idx, state, count, ticket, wp, rows, label, value, coef, scale, top, norm, logit, part, sorted, begin, dx, colsum, dw, total;
+  size_t off, place, part8, once, tb, ub, slot, arcs, nnorm, alpha, beta, dz, de, dp;
 };
 
 void loss_plan(LossPlan &p) {
@@ -207,7 +207,8 @@ void loss_plan(LossPlan &p) {
   p.logit = take(R * p.K * 4);
   p.coef = take(R * p.K * 4);
   p.scale = take(R * 4);
-  p.lse2 = take(R * 4);
+  p.top = take(R * 4);
+  p.norm = take(R * 4);
   p.part = take(R * 8 * p.parts);
   if (p.sort) {
     p.sorted = take(R * p.K * 4);
@@ -226,7 +227,7 @@ void loss_plan(LossPlan &p) {
     p.part8 = take((size_t)p.B * 4);
     p.slot = take(R * 4);
     p.arcs = take((size_t)p.places * 16);
-    p.nlse2 = take(n * 4);
+    p.nnorm = take(n * 8);
   }
   if (p.grads) {
     p.dx = take((size_t)p.pd * R * p.vblk * 64);
@@ -328,7 +329,8 @@ LossPack loss_begin(LossRun &r) {
   k.value = p.kind == kLossDistill ? r.at<float>(p.value) : nullptr;
   k.coef = r.at<float>(p.coef);
   k.scale = r.at<float>(p.scale);
-  k.lse2 = r.at<float>(p.lse2);
+  k.top = r.at<float>(p.top);
+  k.norm = r.at<float>(p.norm);
   k.logit = r.at<float>(p.logit);
   k.part = r.at<float2>(p.part);
   k.parts = p.parts;
@@ -628,7 +630,7 @@ int wind_transducer_loss(const wind_output_layer *layer, const void *e, int64_t 
   l.tb = r.at<int>(p.tb);
   l.ub = r.at<int>(p.ub);
   l.count = r.at<int>(p.count);
-  l.nodes = LossNodes{r.at<float4>(p.arcs), r.at<int>(p.slot), r.at<float>(p.nlse2)};
+  l.nodes = LossNodes{r.at<float4>(p.arcs), r.at<int>(p.slot), r.at<float2>(p.nnorm)};
   l.place = r.at<int>(p.place);
   l.part = r.at<int>(p.part8);
   l.cells = p.cells;

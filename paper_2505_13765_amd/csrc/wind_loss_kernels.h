@@ -13,8 +13,9 @@
 // Everything runs chunk by chunk over the rows that count: rows without a label, or utterances' padding, are left out on the device
 // (how many remain is known there only: workgroups past the end leave at once).
 //
-// Powers of two.  Row statistics are kept in units of log2: with c = log2(e) / tau the largest logit of a block is m = fl(x c), every sum
-// is of exp2(fma(x, c, -m)), and lse2 = m + log2(sum), so that the rounding of m cancels.
+// Exponentials.  A row's statistics are its largest logit m and s = sum exp2((x - m) c), c = log2(e) / tau: the difference is taken before it is scaled, so
+// that the largest term is 1 whatever the logits' size (a block of outputs that the bias masks with -1e30 had a sum of exp2 of m c's rounding, and with the lowest
+// value m c was infinite).  -log2 p = (m - x) c + log2 s, and p itself is exp2((x - m) c - log2 s).
 #pragma once
 #include "wind_loss_gemm.h"
 
@@ -225,7 +226,7 @@ struct LossChunk {
   float *value;                // [K][R] log2 of the teacher's probability (distillation)
   float *coef;                 // [K][R]
   float *scale;                // [R]
-  float *lse2;                 // [R] (+inf: row does not count)
+  float *top, *norm;           // [R] largest logit, log2 of the sum (0, +inf: row does not count)
   float *logit;                // [K][R] the entries' logits
   float2 *part;                // [column blocks][R] (largest, sum)
   // many entries (else null): those of 32 rows by column block, and where each block's begin
@@ -246,7 +247,8 @@ __device__ __forceinline__ void loss_entries(const LossRowsDev &r, const LossChu
       for (int e = l; e < k.K; e += group) k.label[(size_t)e * k.R + i] = -1;
       if (l == 0) {
         k.scale[i] = 0.f;
-        k.lse2[i] = __builtin_inff();
+        k.top[i] = 0.f;
+        k.norm[i] = __builtin_inff();
       }
       continue;
     }
@@ -528,7 +530,7 @@ __device__ __forceinline__ Cell cell_of_log2(float l) {
 struct LossNodes {
   float4 *arcs;                // per place of a lattice node: the probabilities of blank and of its label (m, e, m, e; e as bits)
   int *slot;                   // [R] places of the chunk's nodes
-  float *lse2;                 // per node
+  float2 *norm;                // per node: top and norm as in LossChunk
 };
 // What the workgroups of a row tile leave for the one that joins it (JOIN) goes past their L2s, which do not see each other's.
 template <bool JOIN, class U>
@@ -553,7 +555,7 @@ __device__ __forceinline__ void loss_rows_done(const LossRowsDev &r, const LossC
     for (int p = grp; p < parts; p += G) {
       const float2 v = __builtin_bit_cast(float2, loss_take<JOIN>(reinterpret_cast<const unsigned long long *>(k.part) + (size_t)p * k.R + i));
       const float top = fmaxf(m, v.x), ref = top == -__builtin_inff() ? 0.f : top;
-      s = s * __builtin_amdgcn_exp2f(m - ref) + v.y * __builtin_amdgcn_exp2f(v.x - ref);
+      s = s * __builtin_amdgcn_exp2f((m - ref) * k.c) + v.y * __builtin_amdgcn_exp2f((v.x - ref) * k.c);
       m = top;
     }
   }
@@ -566,27 +568,32 @@ __device__ __forceinline__ void loss_rows_done(const LossRowsDev &r, const LossC
   const float ref = top == -__builtin_inff() ? 0.f : top;
   s = 0.f;
 #pragma unroll 16
-  for (int q = 0; q < G; ++q) s += ss[q * ROWS + lane] * __builtin_amdgcn_exp2f(sm[q * ROWS + lane] - ref);
+  for (int q = 0; q < G; ++q) s += ss[q * ROWS + lane] * __builtin_amdgcn_exp2f((sm[q * ROWS + lane] - ref) * k.c);
   const float ls = log2f(s);
-  // -log2 p of entry e
-  auto cost = [&](int e) { return __builtin_fmaf(-loss_take<JOIN>(k.logit + (size_t)e * k.R + i), k.c, top) + ls; };
+  // how far below the largest logit entry e's is: -log2 p = below c + ls, -log p = below / tau + ls ln 2
+  auto below = [&](int e) { return top - loss_take<JOIN>(k.logit + (size_t)e * k.R + i); };
+  auto cost = [&](int e) { return __builtin_fmaf(below(e), r.inv_tau, ls * (float)kLn2); };
   const bool first = grp == 0 && i < live;
-  if (first) k.lse2[i] = top + ls;
+  if (first) {
+    k.top[i] = top;
+    k.norm[i] = ls;
+  }
   float sum = 0.f;
   if (r.kind == kLossLattice) {
     if (first) {
-      const Cell stay = cell_of_log2(-cost(0)), take = cell_of_log2(k.label[(size_t)k.R + i] < 0 ? -__builtin_inff() : -cost(1));
-      nodes.lse2[k.c0 + i] = top + ls;
+      auto arc = [&](int e) { return cell_of_log2(-__builtin_fmaf(below(e), k.c, ls)); };
+      const Cell stay = arc(0), take = k.label[(size_t)k.R + i] < 0 ? Cell{0.f, kCellZero} : arc(1);
+      nodes.norm[k.c0 + i] = make_float2(top, ls);
       nodes.arcs[nodes.slot[i]] = make_float4(stay.m, __int_as_float(stay.e), take.m, __int_as_float(take.e));
     }
   } else if (r.kind == kLossLabel) {
-    if (first) r.loss[r.idx[k.c0 + i]] = cost(0) * (float)kLn2;
+    if (first) r.loss[r.idx[k.c0 + i]] = cost(0);
   } else {
     if (i < live) {
 #pragma unroll 4
       for (int e = grp; e < k.K; e += G) {
         const float lq = k.value[(size_t)e * k.R + i], q = exp2f(lq);   // (an entry that is not there has q = 0)
-        if (q != 0.f) sum += q * (lq + cost(e));
+        if (q != 0.f) sum += q * __builtin_fmaf(lq, (float)kLn2, cost(e));
       }
     }
     __syncthreads();
@@ -595,7 +602,7 @@ __device__ __forceinline__ void loss_rows_done(const LossRowsDev &r, const LossC
     if (first) {
 #pragma unroll 16
       for (int q = 1; q < G; ++q) sum += sm[q * ROWS + lane];
-      r.loss[r.idx[k.c0 + i]] = sum * (float)kLn2 * r.tau * r.tau;
+      r.loss[r.idx[k.c0 + i]] = sum * r.tau * r.tau;
     }
   }
   __syncthreads();
@@ -630,16 +637,16 @@ __device__ __forceinline__ void loss_stats(const LossProduct &g, const LossChunk
 #pragma unroll
       for (int r = 0; r < 16; ++r) m = fmaxf(m, acc[mi][ni][r]);
     m = fmaxf(m, xor32_f32(m));
-    const float mc = m * k.c, ref = m == -__builtin_inff() ? 0.f : mc;
+    const float ref = m == -__builtin_inff() ? 0.f : m;
     float sum = 0.f;
 #pragma unroll
     for (int ni = 0; ni < T::NI; ++ni)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[mi][ni][r], k.c, -ref));
+      for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f((acc[mi][ni][r] - ref) * k.c);
     sum += xor32_f32(sum);
     if (lane < 32)
       loss_leave<JOIN>(reinterpret_cast<unsigned long long *>(k.part) + (size_t)part * k.R + i,
-                       __builtin_bit_cast(unsigned long long, make_float2(mc, sum)));
+                       __builtin_bit_cast(unsigned long long, make_float2(m, sum)));
     if (entries.hit >> mi & 1u) {
       loss_tile_out<T>(acc[mi], tile);
       if (k.sorted) {
@@ -708,11 +715,11 @@ __device__ __forceinline__ void loss_dx(const LossProduct &g, const LossChunk &k
 #pragma unroll
   for (int mi = 0; mi < T::MI; ++mi) {
     const int i = i0 + 32 * mi;
-    const float s = k.scale[i], lse2 = k.lse2[i];
+    const float s = k.scale[i], top = k.top[i], norm = k.norm[i];
 #pragma unroll
     for (int ni = 0; ni < T::NI; ++ni)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[mi][ni][r] = s * __builtin_amdgcn_exp2f(__builtin_fmaf(acc[mi][ni][r], k.c, -lse2));
+      for (int r = 0; r < 16; ++r) acc[mi][ni][r] = s * __builtin_amdgcn_exp2f(__builtin_fmaf(acc[mi][ni][r] - top, k.c, -norm));
     if (entries.hit >> mi & 1u) {
       loss_tile_out<T>(acc[mi], tile);
       float *row = tile + (lane & 31) * T::PITCH;

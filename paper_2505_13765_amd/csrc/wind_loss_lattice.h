@@ -253,7 +253,8 @@ __device__ __forceinline__ void lattice_chunk(const LatticeDev &l, const LossChu
     if (q == 0 && part == 0) {
       k.label[i] = k.label[k.R + i] = -1;
       k.scale[i] = 0.f;
-      k.lse2[i] = __builtin_inff();
+      k.top[i] = 0.f;
+      k.norm[i] = __builtin_inff();
     }
     return;
   }
@@ -315,7 +316,9 @@ __global__ __launch_bounds__(256) void lattice_counts_kernel(LatticeDev l, LossC
   k.coef[i] = by_blank;
   k.coef[k.R + i] = by_label;
   k.scale[i] = by_blank + by_label;
-  k.lse2[i] = l.nodes.lse2[n];
+  const float2 norm = l.nodes.norm[n];
+  k.top[i] = norm.x;
+  k.norm[i] = norm.y;
 }
 
 // Sums of dz, where z is above zero, over the chunk's rows of one frame (which = 0) or of one prediction row (which = 1): a workgroup takes 256 columns
