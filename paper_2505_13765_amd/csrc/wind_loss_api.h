@@ -189,7 +189,8 @@ void loss_plan(LossPlan &p) {
   p.narrow = loss_narrow((p.pd == 3 ? kLossShapesF32 : kLossShapes)[p.x.shape], p.V1);
   p.fold_once = p.kind == kLossLattice && N * p.hd * 4 >= kLatticeOnce;
   p.sort = p.kind == kLossDistill && p.K > 2 && p.K <= kLossSortMost && N * p.K > kLossSmall && (double)N * p.K * p.parts >= kLossSortWork;
-  p.join = !p.narrow && !p.sort && N * p.K <= kLossJoinEntries && p.parts <= kLossJoinParts;
+  // (one chunk: the tickets by which a row tile's last workgroup is known are cleared once per call)
+  p.join = p.chunks == 1 && !p.narrow && !p.sort && N * p.K <= kLossJoinEntries && p.parts <= kLossJoinParts;
   p.dw_direct = p.chunks == 1 && p.w.splits == 1;
   p.dz_direct = p.kind != kLossLattice && p.z.splits == 1;
   size_t at = 0;

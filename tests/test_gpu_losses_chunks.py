@@ -1,0 +1,73 @@
+"""Losses over the output layer of more rows than a workspace holds at a time.  That a call takes several pieces is asserted from the size of its workspace, which
+is smaller than one piece's rows would be."""
+import ctypes as C
+import math
+
+import pytest
+import torch
+
+from loss_norms import SHARE, near
+from loss_reference import close, row_loss, transducer_loss
+from test_gpu_losses import GRAD, api, check, lattice, rows
+
+pytestmark = pytest.mark.gpu
+
+
+def query(name, w, *sizes):
+    from paper_2505_13765_amd.binding import WIND_BF16, WIND_F32, OutputLayer, load_library
+
+    lay, n = OutputLayer(w.data_ptr(), None, w.shape[1], *w.shape, WIND_BF16 if w.dtype == torch.bfloat16 else WIND_F32), C.c_size_t(0)
+    assert getattr(load_library(), name)(C.byref(lay), *sizes, C.byref(n)) == 0
+    return n.value
+
+
+def row_pieces(w, N, K, grads):
+    """At least so many pieces: bytes of all rows' panels (and of the gradients of logits and, of a lattice, of z) over those of the workspace."""
+    V1, H = w.shape
+    size = 2 if w.dtype == torch.bfloat16 else 6
+    return math.ceil(N * size * (H + (V1 if grads else 0)) / query("wind_row_loss_workspace_bytes", w, N, K, grads))
+
+
+def lattice_pieces(w, B, T, U, grads):
+    V1, H = w.shape
+    rows, dx = (4, 2) if w.dtype == torch.bfloat16 else (6, 6)
+    return math.ceil(B * T * (U + 1) * (rows * H + (dx * V1 + 4 * H if grads else 0)) / query("wind_transducer_loss_workspace_bytes", w, B, T, U, grads))
+
+
+def check_norms(got, ref, names, share):
+    for t, name in zip(got[1:], names):
+        want = ref[name][0]
+        near(t.double().reshape(1, -1), want.reshape(1, -1), share, name)
+        if name in "ehp":
+            near(t, want, share, name + " by block")
+
+
+@pytest.mark.parametrize("grad", (None, ("h", "w", "b")))
+def test_few_wide_rows_in_pieces(grad):
+    """Few rows, few outputs and hidden rows so long that a piece holds part of them: each piece's column blocks are joined by the launch that makes them."""
+    N, H, V1 = 4096, 80000, 300
+    h, w, b, labels, weights = rows(N, H, V1, "f32", 34, left_out=0.0)
+    assert row_pieces(w, N, 1, 0 if grad is None else 1) >= 2
+    ref = row_loss(h, w, b, labels, weights=weights)
+    got = api().label_loss(h, w, b, labels, weights, grad=grad)
+    if grad is None:
+        close(got, *ref["loss"], "loss")
+        return
+    check(got, ref, grad)
+    check_norms(got, ref, grad, SHARE["f32"])
+
+
+@pytest.mark.parametrize("grad", (None, GRAD))
+def test_few_wide_nodes_in_pieces(grad):
+    B, T, U, H = 2, 100, 9, 110000
+    a = lattice(B, T, U, H, 12, "f32", 35)
+    a[0], a[1], a[4] = torch.nan_to_num(a[0]), torch.nan_to_num(a[1], posinf=0.0), a[4].clamp(min=0)
+    a[5][:], a[6][:] = T, U
+    assert lattice_pieces(a[2], B, T, U, 0 if grad is None else 1) >= 2
+    ref = transducer_loss(*a)
+    got = api().transducer_loss(*a, grad=grad)
+    if grad is None:
+        close(got, *ref["loss"], "loss")
+        return
+    check(got, ref, GRAD)
+    check_norms(got, ref, GRAD, SHARE["f32"])
