@@ -369,7 +369,8 @@ int wind_get_route_counts(wind_model *m, wind_route_counts *out);
  *               nothing, does not wait and can be captured.  Calls (and replays of captured ones) that share a workspace must not
  *               overlap in time
  * Sums are formed in a fixed order: the same call gives the same bits.  Returns WIND_ERR_ARG for null pointers, sizes out of
- * range and a missing, misaligned or too small workspace, WIND_ERR_UNSUPPORTED for V1 * H of 2^31 and more, or K above 1024.
+ * range and a missing, misaligned or too small workspace, WIND_ERR_UNSUPPORTED for V1 * H of 2^31 and more (both
+ * rounded up to whole 32), V1 or H above 2^23 - 32, or K above 1024.
  */
 typedef struct {
   const void *w;        /* DEVICE [V1, H]                                  */

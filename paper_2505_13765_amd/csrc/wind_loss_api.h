@@ -34,9 +34,9 @@ struct LossTiles<3, 3> {
   using T1 = LossTile<1, 1, 3, 3, 1, 3, 2>;
 };
 
-// dx and rows of a chunk, about.  A chunk of 2700 rows of 65537 outputs (512 MB) left the products of few tiles: 8.9 ms for 7373 rows,
-// one chunk 7.4
-constexpr size_t kLossChunkBytes = 1200u << 20;
+// dx and rows of a chunk, about, and what its rows' statistics and entries may take beside (65537 outputs: 16 KB a row at most, as do 1024 entries).  A chunk of 2700
+// rows of 65537 outputs (512 MB) left the products of few tiles: 8.9 ms for 7373 rows, one chunk 7.4
+constexpr size_t kLossChunkBytes = 1200u << 20, kLossStatBytes = 512u << 20;
 constexpr int kLossMaxEntries = 1024;
 // Entries (of all rows) and column blocks up to which a row tile's last workgroup joins its column blocks: one launch less, 36 -> 31 us for 16 rows of 1025
 // outputs.  With more, that workgroup is what the others' results wait for (3001 rows of 64 entries: 73 us against 51 and 6).
@@ -174,9 +174,11 @@ void loss_plan(LossPlan &p) {
   p.pw = p.pd = loss_planes(p.dtype);
   if (p.dtype == WIND_BF16 && p.N <= kLossFineRows) p.pd = 2;
   p.pa = p.kind == kLossLattice ? lattice_planes(p.dtype) : loss_planes(p.dtype);
-  const size_t row = (size_t)p.pa * p.hblk * 64 + (p.grads ? (size_t)p.pd * p.vblk * 64 : 0) + (p.kind == kLossLattice && p.grads ? (size_t)p.hd * 4 : 0);
+  // A chunk holds as many rows without gradients as with them: no panel of it has 2^32 bytes, and losses alone need less memory than a step.
+  const size_t row = (size_t)p.pa * p.hblk * 64 + (size_t)p.pd * p.vblk * 64 + (p.kind == kLossLattice ? (size_t)p.hd * 4 : 0);
+  const size_t stat = (size_t)(p.V1 + 63) / 64 * 16 + (size_t)p.K * 16;
   const long long N = std::max(p.N, 1ll);
-  const long long most = std::max<long long>((long long)(kLossChunkBytes / row) / 256 * 256, 256);
+  const long long most = std::max<long long>((long long)std::min(kLossChunkBytes / row, kLossStatBytes / stat) / 256 * 256, 256);
   p.chunks = (int)((N + most - 1) / most);
   p.R = (int)round_up((size_t)((N + p.chunks - 1) / p.chunks), 256);
   p.chunks = (int)((N + p.R - 1) / p.R);
@@ -266,7 +268,7 @@ int loss_workspace_check(const LossPlan &p, const void *ws, size_t bytes) {
 }
 int loss_rows_limits(const LossPlan &p) {
   if (p.K > kLossMaxEntries) return fail(WIND_ERR_UNSUPPORTED, "K must be at most 1024");
-  if ((unsigned long long)p.R * std::max(p.vblk, p.hblk) * 64 >= 1ull << 32) return fail(WIND_ERR_UNSUPPORTED, "V1 and H must be below 2^24");
+  if ((unsigned long long)p.R * std::max(p.vblk, p.hblk) * 64 >= 1ull << 32) return fail(WIND_ERR_UNSUPPORTED, "V1 and H must be at most 2^23 - 32");   // (a panel of 256 rows)
   return WIND_OK;
 }
 

@@ -71,3 +71,24 @@ def test_few_wide_nodes_in_pieces(grad):
         return
     check(got, ref, GRAD)
     check_norms(got, ref, GRAD, SHARE["f32"])
+
+
+@pytest.mark.parametrize("dtype,N,H,V1", [("bf16", 40001, 640, 65537), ("bf16", 900001, 48, 4097), ("f32", 20000, 320, 65537)])
+def test_scores_of_many_rows(dtype, N, H, V1):
+    """Losses alone, of rows that a step takes too: the same bits as its losses, and the first and last rows' against the reference."""
+    h, w, b, labels, weights = rows(N, H, V1, dtype, 37)
+    loss = api().label_loss(h, w, b, labels)
+    assert torch.equal(loss, api().label_loss(h, w, b, labels, weights, grad=("b",))[0])
+    for part in (slice(0, 500), slice(N - 500, N)):
+        close(loss[part], *row_loss(h[part], w, b, labels[part])["loss"], "loss")
+    assert not loss[labels < 0].any() and (loss[labels >= 0] > 0).all()
+
+
+@pytest.mark.parametrize("dtype,B,T,U,H,V1", [("bf16", 16, 750, 120, 640, 8193), ("bf16", 32, 750, 120, 48, 4097), ("f32", 8, 250, 40, 96, 8193)])
+def test_scores_of_many_nodes(dtype, B, T, U, H, V1):
+    a = lattice(B, T, U, H, V1, dtype, 38)
+    loss = api().transducer_loss(*a)
+    assert torch.equal(loss, api().transducer_loss(*a, grad=("b",))[0]) and torch.isfinite(loss).all()
+    for i in (0, B - 1):
+        one = [t[i:i + 1] for t in a[:2]] + a[2:4] + [t[i:i + 1] for t in a[4:]]
+        close(loss[i:i + 1], *transducer_loss(*one)["loss"], "loss")

@@ -1,0 +1,47 @@
+"""What the losses over the output layer take and refuse, and the workspaces they ask for, without a GPU."""
+import ctypes as C
+
+import pytest
+
+from test_losses_cpu import lattice_size, layer, lib, rows_size  # noqa: F401  (lib: the fixture)
+
+
+@pytest.mark.parametrize("V1,H,dtype,N", [(65537, 640, 1, 100000), (65537, 2048, 1, 40000), (50257, 768, 1, 131072), (128256, 4096, 1, 65536), (4097, 640, 1, 900000),
+                                          (4097, 640, 1, 1000000), (65537, 2048, 0, 40000), (33, 48, 1, 50000000), (2, 1, 1, (1 << 31) - 1)])
+def test_scores_of_many_rows_are_taken(lib, V1, H, dtype, N):  # noqa: F811
+    """Whatever a step takes, with less memory than the step."""
+    from paper_2505_13765_amd.binding import WIND_OK
+
+    lay = layer(V1=V1, H=H, dtype=dtype)
+    step, scores = rows_size(lib, lay, N), rows_size(lib, lay, N, grads=0)
+    assert step[0] == scores[0] == WIND_OK and scores[1] <= step[1]
+
+
+@pytest.mark.parametrize("V1,H,dtype,B,T,U", [(8193, 640, 1, 16, 750, 120), (4097, 200, 1, 32, 750, 120), (8193, 48, 1, 32, 750, 120), (8193, 640, 1, 32, 250, 40),
+                                              (1025, 64, 1, 32, 750, 120), (8193, 640, 0, 32, 750, 120), (4097, 640, 1, 16, 750, 120)])
+def test_scores_of_many_nodes_are_taken(lib, V1, H, dtype, B, T, U):  # noqa: F811
+    from paper_2505_13765_amd.binding import WIND_OK
+
+    lay = layer(V1=V1, H=H, dtype=dtype)
+    step, scores = lattice_size(lib, lay, B, T, U), lattice_size(lib, lay, B, T, U, grads=0)
+    assert step[0] == scores[0] == WIND_OK and scores[1] <= step[1]
+
+
+@pytest.mark.parametrize("grads", (0, 1))
+@pytest.mark.parametrize("V1,H,K", [(65537, 64, 1), (1 << 20, 64, 1), (1025, 640, 1024), (33, 32, 1024)])
+def test_workspaces_hold_a_piece(lib, V1, H, K, grads):  # noqa: F811
+    """Rows, statistics and entries of a piece, not of all rows: some bytes a row are all that a workspace grows by."""
+    few, many = (rows_size(lib, layer(V1=V1, H=H, dtype=1), N, K=K, grads=grads)[1] for N in (1 << 22, 1 << 23))
+    assert many < 4 << 30 and many - few <= 8 << 22
+
+
+def test_widths_out_of_range_are_refused(lib):  # noqa: F811
+    from paper_2505_13765_amd.binding import WIND_ERR_UNSUPPORTED, WIND_OK
+
+    most = (1 << 23) - 32
+    for grads in (0, 1):
+        assert rows_size(lib, layer(V1=most, H=32), 8, grads=grads)[0] == WIND_OK
+        assert rows_size(lib, layer(V1=32, H=most), 8, grads=grads)[0] == WIND_OK
+        for bad in (dict(V1=most + 1, H=32), dict(V1=32, H=most + 1)):
+            assert rows_size(lib, layer(**bad), 8, grads=grads)[0] == WIND_ERR_UNSUPPORTED and b"2^23" in lib.wind_last_error()
+            assert lattice_size(lib, layer(**bad), 1, 4, 2, grads=grads)[0] == WIND_ERR_UNSUPPORTED
