@@ -34,12 +34,52 @@ def lattice_pieces(w, B, T, U, grads):
     return math.ceil(B * T * (U + 1) * (rows * H + (dx * V1 + 4 * H if grads else 0)) / query("wind_transducer_loss_workspace_bytes", w, B, T, U, grads))
 
 
+def row_reference(h, w, b, labels, logits=None, tau=1.0, weights=None, step=3000):
+    """row_loss, piece by piece: its fp64 logits of all rows would not fit."""
+    part = lambda t, i: None if t is None else t[i:i + step]  # noqa: E731
+    refs = [row_loss(part(h, i), w, b, part(labels, i), part(logits, i), tau, part(weights, i)) for i in range(0, len(h), step)]
+    out = {k: tuple(torch.cat([r[k][x] for r in refs]) for x in range(2)) for k in ("loss", "h")}
+    for k in ("w", "b"):
+        value = sum(r[k][0] for r in refs)
+        out[k] = value, sum(r[k][1] for r in refs) + 2.0 ** -24 * len(refs) * value.abs()   # (added up once more per piece)
+    return out
+
+
 def check_norms(got, ref, names, share):
     for t, name in zip(got[1:], names):
         want = ref[name][0]
         near(t.double().reshape(1, -1), want.reshape(1, -1), share, name)
         if name in "ehp":
             near(t, want, share, name + " by block")
+
+
+@pytest.mark.parametrize("dtype,N,H,V1", [("bf16", 24001, 64, 65537), ("f32", 16001, 96, 30001)])
+def test_label_loss_in_pieces(dtype, N, H, V1):
+    """A last piece of few rows, and pieces without any row that counts."""
+    h, w, b, labels, weights = rows(N, H, V1, dtype, 31, left_out=0.0)
+    assert row_pieces(w, N, 1, 1) >= 2
+    for end in (N, N // 3, 0):
+        labels[end:] = -1
+        ref = row_reference(h, w, b, labels, weights=weights)
+        got = api().label_loss(h, w, b, labels, weights, grad=("h", "w", "b"))
+        check(got, ref, "hwb")
+        check_norms(got, ref, "hwb", SHARE[dtype])
+
+
+@pytest.mark.parametrize("dtype,N,H,V1,K", [("bf16", 14001, 48, 65537, 4), ("bf16", 30001, 64, 30001, 16), ("f32", 12001, 64, 20001, 6)])
+def test_distill_loss_in_pieces(dtype, N, H, V1, K):
+    """Sorted entries of a later piece among them."""
+    h, w, b, _, weights = rows(N, H, V1, dtype, 32, left_out=0.0)
+    assert row_pieces(w, N, K, 1) >= 2
+    g = torch.Generator().manual_seed(33)
+    labels = torch.randint(-1, V1, (N, K), generator=g, dtype=torch.int32)
+    labels[::3, 1] = labels[::3, 0]
+    logits = 2 * torch.randn((N, K), generator=g)
+    labels, logits = labels.cuda(), logits.cuda()
+    ref = row_reference(h, w, b, labels, logits, 2.0, weights)
+    got = api().distill_loss(h, w, b, labels, logits, 2.0, weights, grad=("h", "w", "b"))
+    check(got, ref, "hwb")
+    check_norms(got, ref, "hwb", SHARE[dtype])
 
 
 @pytest.mark.parametrize("grad", (None, ("h", "w", "b")))
@@ -92,3 +132,32 @@ def test_scores_of_many_nodes(dtype, B, T, U, H, V1):
     for i in (0, B - 1):
         one = [t[i:i + 1] for t in a[:2]] + a[2:4] + [t[i:i + 1] for t in a[4:]]
         close(loss[i:i + 1], *transducer_loss(*one)["loss"], "loss")
+
+
+@pytest.mark.parametrize("dtype,B,T,U,H,V1", [("bf16", 24, 400, 60, 64, 2049), ("f32", 8, 250, 40, 32, 4097), ("bf16", 3, 2000, 60, 65, 3001)])
+def test_lattices_in_pieces(dtype, B, T, U, H, V1):
+    """Frames and labels whose sums go over a piece's end, utterances that end early or do not count, pieces without nodes; with dz read once and apart."""
+    a = lattice(B, T, U, H, V1, dtype, 36)
+    a[0], a[1], a[4] = torch.nan_to_num(a[0]), torch.nan_to_num(a[1], posinf=0.0), a[4].clamp(min=0)
+    a[5][:], a[6][:] = T, U
+    assert lattice_pieces(a[2], B, T, U, 1) >= 2
+    a[5][1], a[6][2] = T // 2 + 3, U // 3
+    for shorter in (False, True):
+        if shorter:
+            a[5][1:] = 0
+            a[5][0] = T // 3
+        ref = transducer_loss(*a)
+        got = api().transducer_loss(*a, grad=GRAD)
+        check(got, ref, GRAD)
+        check_norms(got, ref, GRAD, SHARE[dtype])
+        for part in (("e",), ("p",)):       # (the folds apart)
+            some = api().transducer_loss(*a, grad=part)
+            check_norms(some, ref, part, SHARE[dtype])
+
+
+def test_a_large_lattice_in_one_piece():
+    """dz read once for both of its folds: shares of the norms, frame by frame and prediction row by prediction row."""
+    a = lattice(3, 203, 40, 701, 40, "bf16", 16)
+    a[0], a[1], a[4] = torch.nan_to_num(a[0]), torch.nan_to_num(a[1], posinf=0.0), a[4].clamp(min=0)
+    a[5][1] = 0
+    check_norms(api().transducer_loss(*a, grad=GRAD), transducer_loss(*a), GRAD, SHARE["bf16"])
