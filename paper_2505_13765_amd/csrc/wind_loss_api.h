@@ -51,11 +51,6 @@ constexpr int kLatticeLong = 64;
 constexpr long long kLatticeOnce = 64ll << 20;   // bytes of dz from which it is read once for both folds, at the price of a launch
 constexpr long long kLatticeFew = 1024;
 
-// Rows up to which dx of bf16 operands keeps 16 bits (two planes) for its products: their gradients are decided by a few values, whose roundings to 8 bits do not
-// average out: 13 rows of 29052 outputs, error of dz 0.0037 of its norm with one plane, 0.0016, the result's own rounding, with two.  The second plane costs 0 to 7 % of
-// a step up to 128 rows, 15 % of one of 256 rows of 65537.
-constexpr long long kLossFineRows = 128;
-
 // the bf16 planes that make up a stored value of each type, and the sum of two bf16 values (hidden rows of the lattice)
 int loss_planes(int dtype) { return dtype == WIND_BF16 ? 1 : 3; }
 int lattice_planes(int dtype) { return dtype == WIND_BF16 ? 2 : 3; }
@@ -233,7 +228,7 @@ void loss_plan(LossPlan &p) {
     p.nnorm = take(n * 8);
   }
   if (p.grads) {
-    p.dx = take((size_t)p.pd * R * p.vblk * 64);
+    p.dx = take(std::max<size_t>(p.pd * R, p.dtype == WIND_BF16 ? 2 * kLossFinePanel : 0) * p.vblk * 64);
     p.colsum = take(2 * ((R + p.x.bm - 1) / p.x.bm) * p.vblk * 128);
     p.dw = p.dw_direct ? at : take((size_t)p.w.splits * p.V1 * p.hd * 4);
     p.dz = p.dz_direct ? at : take((size_t)p.z.splits * R * p.hd * 4);
@@ -292,19 +287,22 @@ void loss_with_tile(int pa, int shape, F &&f) {
     else f(LossTiles<1, 1>::T3{});
   }
 }
-// products of dx: no sums of two values among them
+// products of dx: the tile, and that for dx on two planes where few rows turn out to count
 template <class F>
 void loss_with_dx_tile(int pd, int shape, F &&f) {
+  using One = LossTiles<1, 1>;
+  using Two = LossTiles<2, 1>;
+  using Three = LossTiles<3, 3>;
   if (pd == 3) {
-    if (shape == 0) f(LossTiles<3, 3>::T0{});
-    else f(LossTiles<3, 3>::T1{});
+    if (shape == 0) f(Three::T0{}, Three::T0{});
+    else f(Three::T1{}, Three::T1{});
   } else if (pd == 2) {
-    if (shape == 2) f(LossTiles<2, 1>::T2{});
-    else f(LossTiles<2, 1>::T3{});
-  } else if (shape == 0) f(LossTiles<1, 1>::T0{});
-  else if (shape == 1) f(LossTiles<1, 1>::T1{});
-  else if (shape == 2) f(LossTiles<1, 1>::T2{});
-  else f(LossTiles<1, 1>::T3{});
+    if (shape == 2) f(Two::T2{}, Two::T2{});
+    else f(Two::T3{}, Two::T3{});
+  } else if (shape == 0) f(One::T0{}, Two::T0{});
+  else if (shape == 1) f(One::T1{}, Two::T1{});
+  else if (shape == 2) f(One::T2{}, Two::T2{});
+  else f(One::T3{}, Two::T3{});
 }
 
 struct LossRun {                     // what the launches of one call share
@@ -377,7 +375,7 @@ void loss_stats(const LossRun &r, LossNodes nodes) {
 LossFinish loss_gradients(const LossRun &r, int chunk, bool dz, LossOut dz_out, void *dw, float *db) {
   const LossPlan &p = r.p;
   const LossProduct g = loss_logits(r);
-  const LossDx d{r.at<bf16_t>(p.dx), (size_t)p.R * p.vblk * 32, p.pd, p.vblk, db ? r.at<float>(p.colsum) : nullptr};
+  const LossDx d{r.at<bf16_t>(p.dx), (size_t)p.R * p.vblk * 32, p.pd, p.vblk, db ? r.at<float>(p.colsum) : nullptr, p.pd == 1};
   loss_with_tile(p.pa, p.x.shape, [&](auto t) {
     using T = decltype(t);
     const unsigned grid = loss_grid((p.R + T::BM - 1) / T::BM, g.ct);
@@ -410,8 +408,8 @@ LossFinish loss_gradients(const LossRun &r, int chunk, bool dz, LossOut dz_out, 
   const unsigned z_blocks = dz ? loss_grid((p.R + p.z.bm - 1) / p.z.bm, z.ct, zo.splits) : 0;
   const unsigned w_blocks = dw ? loss_grid((p.V1 + p.w.bm - 1) / p.w.bm, w.ct, wo.splits) : 0;
   if (dz || dw)
-    loss_with_dx_tile(p.pd, p.z.shape, [&](auto t) {
-      loss_products_kernel<decltype(t)><<<z_blocks + w_blocks, 256, 0, r.s>>>(z, zo, (int)z_blocks, w, wo, r.chunk);
+    loss_with_dx_tile(p.pd, p.z.shape, [&](auto t, auto fine) {
+      loss_products_kernel<decltype(t), decltype(fine)><<<z_blocks + w_blocks, 256, 0, r.s>>>(z, zo, (int)z_blocks, w, wo, r.chunk);
     });
   return f;
 }

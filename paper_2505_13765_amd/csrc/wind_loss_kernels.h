@@ -692,13 +692,22 @@ __global__ __launch_bounds__(256, T::W) void loss_stats_kernel(LossProduct g, Lo
     for (int i = ti * T::BM; i < end; i += 64) loss_rows_done<64, true>(r, k, end, parts, nodes, i, sm);
 }
 
+// Rows that count in all up to which dx of bf16 operands is kept on 16 bits (two planes) for its products: gradients of few rows are decided by a few values of it, whose
+// roundings to 8 bits do not average out (13 rows of 29052 outputs: error of dz 0.0037 of its norm with one plane, 0.0016, the result's own rounding, with two).  The
+// second plane costs 0 to 7 % of a step up to 128 rows, 15 % of one of 256 rows of 65537.
+constexpr int kLossFineRows = 128;
+
 // dx of a chunk, in panels, and its column sums.
 struct LossDx {
   bf16_t *dx;
   size_t plane;
   int planes, blocks;
   float *colsum;               // [2 row tiles][blocks * 32] sums over a wave's rows, or null
+  int may_fine;                // one plane; two, of 256 rows each, where no more rows count than kLossFineRows
 };
+// The row tiles of few rows end at 256 at the latest, and the space of one plane of all rows (512 at least) holds both of theirs.
+constexpr int kLossFinePanel = 256;
+__device__ __forceinline__ bool loss_fine(int may_fine, const LossChunk &k) { return may_fine && *k.count <= kLossFineRows; }
 
 template <class T>
 __device__ __forceinline__ void loss_dx(const LossProduct &g, const LossChunk &k, const float *bias, const LossDx &d, int row0, int j0, int part0, unsigned char *smem) {
@@ -712,6 +721,9 @@ __device__ __forceinline__ void loss_dx(const LossProduct &g, const LossChunk &k
     loss_bias<T>(bias, g.cols, col0, acc);
   });
   float *tile = reinterpret_cast<float *>(smem) + wave * 32 * T::PITCH;
+  const bool fine = loss_fine(d.may_fine, k);
+  const int planes = fine ? 2 : d.planes;
+  const size_t panel = (size_t)(fine ? kLossFinePanel : k.R) * 32, plane = fine ? panel * d.blocks : d.plane;
 #pragma unroll
   for (int mi = 0; mi < T::MI; ++mi) {
     const int i = i0 + 32 * mi;
@@ -784,18 +796,18 @@ __device__ __forceinline__ void loss_dx(const LossProduct &g, const LossChunk &k
         float rest[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) rest[j] = acc[mi][ni][8 * q + j];
-        for (int p = 0; p < d.planes; ++p) {
+        for (int p = 0; p < planes; ++p) {
           uint32_t w[4];
 #pragma unroll
           for (int j = 0; j < 4; ++j) w[j] = pack_bf16x2(rest[2 * j], rest[2 * j + 1]);
-          if (p + 1 < d.planes) {
+          if (p + 1 < planes) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) rest[j] -= __uint_as_float((j & 1) ? (w[j >> 1] & 0xFFFF0000u) : (w[j >> 1] << 16));
           }
           const auto x = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
           const auto y = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
           const u32x4 out = {(uint32_t)x[0], (uint32_t)y[0], (uint32_t)x[1], (uint32_t)y[1]};
-          *reinterpret_cast<u32x4 *>(d.dx + (size_t)p * d.plane + (size_t)blk * k.R * 32 + (size_t)i * 32 + (2 * q + half) * 8) = out;
+          *reinterpret_cast<u32x4 *>(d.dx + (size_t)p * plane + (size_t)blk * panel + (size_t)i * 32 + (2 * q + half) * 8) = out;
         }
       }
     }
@@ -918,11 +930,25 @@ __device__ __forceinline__ void loss_product(int bid, const LossProduct &g, cons
 // dz = dx W: rows of the chunk against columns of W's panels, summed over outputs.  dW = dx^T z: columns of dx's panels against columns of z's, summed over
 // the chunk's rows.  In one launch, on tiles of one shape.
 template <class T>
-__global__ __launch_bounds__(256, T::W) void loss_products_kernel(LossProduct z, LossOut zo, int z_blocks, LossProduct w, LossOut wo, LossChunk k) {
-  __shared__ __attribute__((aligned(256))) unsigned char smem[T::SMEM];
-  const int live = chunk_rows(k);
+__device__ __forceinline__ void loss_products(const LossProduct &z, const LossOut &zo, int z_blocks, const LossProduct &w, const LossOut &wo, int live, unsigned char *smem) {
   if ((int)blockIdx.x < z_blocks) loss_product<T, false, true>((int)blockIdx.x, z, zo, live, z.slabs, smem);
   else if (!wo.add || live) loss_product<T, true, true>((int)blockIdx.x - z_blocks, w, wo, w.cols, (live + 31) / 32, smem);
+}
+// F: the tile of the same shape for dx on two planes, where that is decided by the rows that count; else T.
+template <class T, class F>
+__global__ __launch_bounds__(256, T::W) void loss_products_kernel(LossProduct z, LossOut zo, int z_blocks, LossProduct w, LossOut wo, LossChunk k) {
+  static_assert(F::BM == T::BM && F::BN == T::BN && F::W == T::W, "one grid for both");
+  __shared__ __attribute__((aligned(256))) unsigned char smem[F::SMEM > T::SMEM ? F::SMEM : T::SMEM];
+  const int live = chunk_rows(k);
+  if constexpr (F::PA != T::PA) {
+    if (loss_fine(1, k)) {
+      z.a.rows = w.a.rows = kLossFinePanel;
+      z.a.plane = w.a.plane = (size_t)kLossFinePanel * 32 * z.a.blocks;
+      loss_products<F>(z, zo, z_blocks, w, wo, live, smem);
+      return;
+    }
+  }
+  loss_products<T>(z, zo, z_blocks, w, wo, live, smem);
 }
 
 // ---- the last launch of a chunk -----------------------------------------------------------------

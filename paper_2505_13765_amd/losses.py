@@ -2,7 +2,7 @@
 wind_transducer_loss (include/wind.h says what they compute).  Argument checks and output tensors only.
 
 The output layer is given as tensors on the GPU: w_out [V1, H] in float32 or bfloat16 and b_out [V1] in float32 or None, blank the last
-output.  Rows have w_out's type.  Every tensor of a call lies on one device; the kernels are enqueued on that device's current
+output.  Rows have w_out's type (bfloat16 also rounds the logits' gradient before its products: include/wind.h).  Every tensor of a call lies on one device; the kernels are enqueued on that device's current
 stream, and nothing waits, allocates outside torch or comes back to the host, so calls can be captured into graphs.
 
 Each function returns the losses, or, with `grad` (names of the inputs whose gradients are wanted), a tuple of the losses and
