@@ -367,8 +367,9 @@ int wind_get_route_counts(wind_model *m, wind_route_counts *out);
  *   weights     DEVICE fp32, may be NULL (ones): the gradients are those of the sum over rows (utterances) of weight x loss; the
  *               losses themselves are not weighted
  *   dh, de, dp, dw, db   DEVICE, dense, any of them may be NULL (not wanted); they are overwritten
- *   workspace   DEVICE, 256-byte aligned, at least as many bytes as the query of the same shape says (grads = 1 if a gradient
- *               is wanted); contents on entry do not matter.  The call enqueues its kernels on `stream` and returns; it allocates
+ *   workspace   DEVICE, 256-byte aligned, at least as many bytes as the query says for this layer's V1, H and dtype, K, and at least these
+ *               numbers of rows (of utterances, frames and labels; grads = 1 if a gradient is wanted): one for the largest call, with gradients, serves
+ *               all of them; contents on entry do not matter.  The call enqueues its kernels on `stream` and returns; it allocates
  *               nothing, does not wait and can be captured.  Calls (and replays of captured ones) that share a workspace must not
  *               overlap in time
  * Sums are formed in a fixed order: the same call gives the same bits.  Returns WIND_ERR_ARG for null pointers, sizes out of

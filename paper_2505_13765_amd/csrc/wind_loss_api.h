@@ -91,6 +91,7 @@ constexpr ProductShape kProductShapes[] = {
     {256, 256, 1, 7.0e6, 1.0, 12, 3.2e9}, {256, 128, 2, 8.7e6, 0.73, 10, 1.53e9}, {128, 128, 2, 8.2e6, 0.81, 12, 1.17e9}, {64, 64, 1, 2.2e6, 1.0, 10, 1.6e9}};
 constexpr ProductShape kProductShapesF32[] = {{128, 128, 1, 7.6e6, 1.0, 37, 1.64e9}, {64, 64, 2, 6.5e6, 0.56, 18, 1.1e9}};
 constexpr int kProductParts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+constexpr size_t kLossPartBytes = 80u << 20;   // parts of a sum, at most (of the same 70 problems and 600 others none was picked that takes more than 70 MB)
 
 // when `slots` workgroups at a time end that take nz tiles of time a each, then nw of time b
 double products_end(long long nz, double a, long long nw, double b, long long slots) {
@@ -108,7 +109,7 @@ double products_end(long long nz, double a, long long nw, double b, long long sl
   }
   return std::max(end, hi);
 }
-void products_pick(int planes, long long m, long long V1, long long H, LossPick &z, LossPick &w) {
+void products_pick(int planes, long long m, long long V1, long long H, size_t z_part, size_t w_part, LossPick &z, LossPick &w) {
   const ProductShape *shapes = planes == 3 ? kProductShapesF32 : kProductShapes;
   const int count = planes == 3 ? 2 : 4, products = planes == 3 ? 6 : planes;
   const long long z_slabs = (V1 + 31) / 32, w_slabs = (m + 31) / 32;
@@ -122,10 +123,10 @@ void products_pick(int planes, long long m, long long V1, long long H, LossPick 
     const double slab = (double)s.bm * s.bn * 64 / s.rate, chip = 4.0 * (double)m * (double)H * (double)V1 * products / s.chip;
     const long long most = 1024 * s.pair;
     for (const int pz : kProductParts) {
-      if (pz > 1 && (z_slabs / pz < 8 || z_tiles * pz > most)) break;
+      if (pz > 1 && (z_slabs / pz < 8 || z_tiles * pz > most || pz * z_part > kLossPartBytes)) break;
       const double a = ((double)((z_slabs + pz - 1) / pz) * products + s.start) * slab, z_join = join(pz, m);
       for (const int pw : kProductParts) {
-        if (pw > 1 && (w_slabs / pw < 8 || w_tiles * pw > most)) break;
+        if (pw > 1 && (w_slabs / pw < 8 || w_tiles * pw > most || pw * w_part > kLossPartBytes)) break;
         const double b = ((double)((w_slabs + pw - 1) / pw) * products + s.start) * slab;
         const long long nz = z_tiles * pz, nw = w_tiles * pw;
         double time = s.pair == 1      ? products_end(nz, a, nw, b, 256)
@@ -147,7 +148,7 @@ struct LossPlan {
   long long N;                       // rows at most
   bool grads;
   int B, T, U, cells, skew;          // lattice
-  long long places;
+  size_t places;                     // of the lattice's nodes, at most
   // derived
   int R, chunks, vblk, hblk, hd, pa, pw, pd;
   LossPick x, z, w;                  // logits, dz, dW
@@ -181,24 +182,29 @@ void loss_plan(LossPlan &p) {
   p.x = loss_pick(p.pa, m, p.V1, p.hblk);
   // (of the cells of a padded batch about two thirds count, where its utterances' lengths lie between half of the longest and the whole; chunks but
   // the last are full of cells that count)
-  if (p.grads) products_pick(p.pd, p.kind == kLossLattice && p.B > 1 && p.chunks == 1 ? std::max(m * 2 / 3, 1ll) : m, p.V1, p.H, p.z, p.w);
+  if (p.grads) products_pick(p.pd, p.kind == kLossLattice && p.B > 1 && p.chunks == 1 ? std::max(m * 2 / 3, 1ll) : m, p.V1, p.H, (size_t)p.R * p.hd * 4, (size_t)p.V1 * p.hd * 4, p.z, p.w);
   p.parts = 2 * ((p.V1 + p.x.bn - 1) / p.x.bn);
   p.narrow = loss_narrow((p.pd == 3 ? kLossShapesF32 : kLossShapes)[p.x.shape], p.V1);
   p.fold_once = p.kind == kLossLattice && N * p.hd * 4 >= kLatticeOnce;
-  p.sort = p.kind == kLossDistill && p.K > 2 && p.K <= kLossSortMost && N * p.K > kLossSmall && (double)N * p.K * p.parts >= kLossSortWork;
+  const bool may_sort = p.kind == kLossDistill && p.K > 2 && p.K <= kLossSortMost && N * p.K > kLossSmall;
+  p.sort = may_sort && (double)N * p.K * p.parts >= kLossSortWork;
   // (one chunk: the tickets by which a row tile's last workgroup is known are cleared once per call)
   p.join = p.chunks == 1 && !p.narrow && !p.sort && N * p.K <= kLossJoinEntries && p.parts <= kLossJoinParts;
   p.dw_direct = p.chunks == 1 && p.w.splits == 1;
   p.dz_direct = p.kind != kLossLattice && p.z.splits == 1;
+  // The workspace.  Its size does not fall where N (or B, T, U) rises: what depends on the tiles picked is taken at its most for any number of rows up to N, a chunk's rows
+  // likewise, so that a caller's buffer for the largest call serves the others.
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t here = at;
     at += round_up(bytes, 256);
     return here;
   };
-  const size_t R = (size_t)p.R, n = (size_t)N;
+  const size_t R = std::min<size_t>(round_up((size_t)N, 256), (size_t)most), n = (size_t)N, parts = (size_t)(p.V1 + 63) / 64 * 2;
+  // parts of a sum of `slabs` of which one has `bytes`
+  auto split = [&](size_t slabs, size_t bytes) { return slabs >= 16 ? std::min(std::min<size_t>(slabs / 8, 64) * bytes, kLossPartBytes) : 0; };
   p.count = take(4);
-  p.ticket = take((size_t)p.R / 64 * 4);
+  p.ticket = take(R / 64 * 4);
   p.wp = take((size_t)p.pw * p.vblk * 32 * p.hblk * 64);
   p.rows = take((size_t)p.pa * R * p.hblk * 64);
   p.label = take(R * p.K * 4);
@@ -207,10 +213,10 @@ void loss_plan(LossPlan &p) {
   p.scale = take(R * 4);
   p.top = take(R * 4);
   p.norm = take(R * 4);
-  p.part = take(R * 8 * p.parts);
-  if (p.sort) {
+  p.part = take(R * 8 * parts);
+  if (may_sort) {
     p.sorted = take(R * p.K * 4);
-    p.begin = take(R / 32 * ((size_t)p.parts + 1) * 4);
+    p.begin = take(R / 32 * (parts + 1) * 4);
   }
   if (p.kind != kLossLattice) {
     p.idx = take(n * 4);
@@ -224,19 +230,20 @@ void loss_plan(LossPlan &p) {
     p.place = take((size_t)p.B * 4);
     p.part8 = take((size_t)p.B * 4);
     p.slot = take(R * 4);
-    p.arcs = take((size_t)p.places * 16);
+    p.arcs = take(p.places * 16);
     p.nnorm = take(n * 8);
   }
   if (p.grads) {
-    p.dx = take(std::max<size_t>(p.pd * R, p.dtype == WIND_BF16 ? 2 * kLossFinePanel : 0) * p.vblk * 64);
-    p.colsum = take(2 * ((R + p.x.bm - 1) / p.x.bm) * p.vblk * 128);
-    p.dw = p.dw_direct ? at : take((size_t)p.w.splits * p.V1 * p.hd * 4);
-    p.dz = p.dz_direct ? at : take((size_t)p.z.splits * R * p.hd * 4);
+    p.dx = take((p.dtype == WIND_BF16 ? std::max<size_t>(R, 2 * kLossFinePanel) : 3 * R) * p.vblk * 64);
+    p.colsum = take(R / 64 * 2 * p.vblk * 128);
+    const size_t dw = (size_t)p.V1 * p.hd * 4, dz = R * p.hd * 4;
+    p.dw = take(std::max(n > R ? dw : 0, split(R / 32, dw)));
+    p.dz = take(std::max(p.kind == kLossLattice ? dz : 0, split(p.vblk, dz)));
     if (p.kind == kLossLattice) {
       if (p.fold_once) p.once = take((R / kFoldFrames + (size_t)(p.B + 2) * (p.U + 1)) * p.hd * 4);
-      p.alpha = take((size_t)p.places * 8);
-      p.beta = take((size_t)p.places * 8);
-      if (p.chunks > 1) {
+      p.alpha = take(p.places * 8);
+      p.beta = take(p.places * 8);
+      if (n > R) {
         p.de = take((size_t)p.B * p.T * p.hd * 4);
         p.dp = take((size_t)p.B * (p.U + 1) * p.hd * 4);
       }
@@ -505,9 +512,8 @@ int lattice_plan(LossPlan &p, const wind_output_layer *layer, int B, int T, int 
   p.U = U;
   p.N = (long long)B * T * (U + 1);
   p.cells = U < 64 ? 1 : U < 128 ? 2 : U < 256 ? 4 : U < 1024 ? 1 : 4;   // of a thread of lattice_sums_kernel
-  p.places = (long long)B * (T + U / p.cells) * (U + 1);
-  p.skew = U <= T && p.places < 1ll << 31;
-  if (!p.skew) p.places = p.N;
+  p.skew = U <= T && (long long)B * (T + U / p.cells) * (U + 1) < 1ll << 31;
+  p.places = (size_t)B * ((size_t)T + std::min(T, U)) * ((size_t)U + 1);   // (skewed or not, and whatever the cells of a thread)
   p.grads = grads;
   loss_plan(p);
   return loss_rows_limits(p);

@@ -1,7 +1,6 @@
-"""Losses over the output layer of more rows than a workspace holds at a time.  That a call takes several pieces is asserted from the size of its workspace, which
-is smaller than one piece's rows would be."""
+"""Losses over the output layer of more rows than a workspace holds at a time.  That a call takes several pieces is asserted from its workspace, which does
+not grow with the rows any more."""
 import ctypes as C
-import math
 
 import pytest
 import torch
@@ -21,17 +20,18 @@ def query(name, w, *sizes):
     return n.value
 
 
-def row_pieces(w, N, K, grads):
-    """At least so many pieces: bytes of all rows' panels (and of the gradients of logits and, of a lattice, of z) over those of the workspace."""
+def rows_in_pieces(w, N, K, grads):
+    """Whether a sixteenth of the rows adds less than a tenth of its panels' bytes: the workspace held no more rows before."""
     V1, H = w.shape
-    size = 2 if w.dtype == torch.bfloat16 else 6
-    return math.ceil(N * size * (H + (V1 if grads else 0)) / query("wind_row_loss_workspace_bytes", w, N, K, grads))
+    sizes = [query("wind_row_loss_workspace_bytes", w, n, K, grads) for n in (N * 15 // 16, N)]
+    return sizes[1] - sizes[0] < N // 16 * (2 if w.dtype == torch.bfloat16 else 6) * (H + (V1 if grads else 0)) / 10
 
 
-def lattice_pieces(w, B, T, U, grads):
+def nodes_in_pieces(w, B, T, U, grads):
     V1, H = w.shape
-    rows, dx = (4, 2) if w.dtype == torch.bfloat16 else (6, 6)
-    return math.ceil(B * T * (U + 1) * (rows * H + (dx * V1 + 4 * H if grads else 0)) / query("wind_transducer_loss_workspace_bytes", w, B, T, U, grads))
+    sizes = [query("wind_transducer_loss_workspace_bytes", w, B, t, U, grads) for t in (T * 15 // 16, T)]
+    z, dx = (4, 2) if w.dtype == torch.bfloat16 else (6, 6)
+    return sizes[1] - sizes[0] < B * (T // 16) * (U + 1) * (z * H + (dx * V1 + 4 * H if grads else 0)) / 10
 
 
 def row_reference(h, w, b, labels, logits=None, tau=1.0, weights=None, step=3000):
@@ -57,7 +57,7 @@ def check_norms(got, ref, names, share):
 def test_label_loss_in_pieces(dtype, N, H, V1):
     """A last piece of few rows, and pieces without any row that counts."""
     h, w, b, labels, weights = rows(N, H, V1, dtype, 31, left_out=0.0)
-    assert row_pieces(w, N, 1, 1) >= 2
+    assert rows_in_pieces(w, N, 1, 1)
     for end in (N, N // 3, 0):
         labels[end:] = -1
         ref = row_reference(h, w, b, labels, weights=weights)
@@ -70,7 +70,7 @@ def test_label_loss_in_pieces(dtype, N, H, V1):
 def test_distill_loss_in_pieces(dtype, N, H, V1, K):
     """Sorted entries of a later piece among them."""
     h, w, b, _, weights = rows(N, H, V1, dtype, 32, left_out=0.0)
-    assert row_pieces(w, N, K, 1) >= 2
+    assert rows_in_pieces(w, N, K, 1)
     g = torch.Generator().manual_seed(33)
     labels = torch.randint(-1, V1, (N, K), generator=g, dtype=torch.int32)
     labels[::3, 1] = labels[::3, 0]
@@ -87,7 +87,7 @@ def test_few_wide_rows_in_pieces(grad):
     """Few rows, few outputs and hidden rows so long that a piece holds part of them: each piece's column blocks are joined by the launch that makes them."""
     N, H, V1 = 4096, 80000, 300
     h, w, b, labels, weights = rows(N, H, V1, "f32", 34, left_out=0.0)
-    assert row_pieces(w, N, 1, 0 if grad is None else 1) >= 2
+    assert rows_in_pieces(w, N, 1, 0 if grad is None else 1)
     ref = row_loss(h, w, b, labels, weights=weights)
     got = api().label_loss(h, w, b, labels, weights, grad=grad)
     if grad is None:
@@ -103,7 +103,7 @@ def test_few_wide_nodes_in_pieces(grad):
     a = lattice(B, T, U, H, 12, "f32", 35)
     a[0], a[1], a[4] = torch.nan_to_num(a[0]), torch.nan_to_num(a[1], posinf=0.0), a[4].clamp(min=0)
     a[5][:], a[6][:] = T, U
-    assert lattice_pieces(a[2], B, T, U, 0 if grad is None else 1) >= 2
+    assert nodes_in_pieces(a[2], B, T, U, 0 if grad is None else 1)
     ref = transducer_loss(*a)
     got = api().transducer_loss(*a, grad=grad)
     if grad is None:
@@ -140,7 +140,7 @@ def test_lattices_in_pieces(dtype, B, T, U, H, V1):
     a = lattice(B, T, U, H, V1, dtype, 36)
     a[0], a[1], a[4] = torch.nan_to_num(a[0]), torch.nan_to_num(a[1], posinf=0.0), a[4].clamp(min=0)
     a[5][:], a[6][:] = T, U
-    assert lattice_pieces(a[2], B, T, U, 1) >= 2
+    assert nodes_in_pieces(a[2], B, T, U, 1)
     a[5][1], a[6][2] = T // 2 + 3, U // 3
     for shorter in (False, True):
         if shorter:
@@ -161,3 +161,35 @@ def test_a_large_lattice_in_one_piece():
     a[0], a[1], a[4] = torch.nan_to_num(a[0]), torch.nan_to_num(a[1], posinf=0.0), a[4].clamp(min=0)
     a[5][1] = 0
     check_norms(api().transducer_loss(*a, grad=GRAD), transducer_loss(*a), GRAD, SHARE["bf16"])
+
+
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+def test_one_workspace_for_all_calls(dtype):
+    """A buffer for the largest call, with whatever the last one left in it, serves smaller ones and scores: the same bits as with one of the call's own size."""
+    from paper_2505_13765_amd.binding import WIND_BF16, WIND_F32, OutputLayer, load_library
+
+    lib, most, H, V1 = load_library(), 12000, 200, 5000
+    h, w, b, labels, weights = rows(most, H, V1, dtype, 39)
+    lay = OutputLayer(w.data_ptr(), b.data_ptr(), H, V1, H, WIND_BF16 if dtype == "bf16" else WIND_F32)
+    size = query("wind_row_loss_workspace_bytes", w, most, 1, 1)
+    ws = torch.full((size,), 0xFF, dtype=torch.uint8, device="cuda")
+    for N in (12000, 11000, 3000, 257, 128, 1, 9999):
+        for grad in (("h", "w", "b"), None):
+            want = api().label_loss(h[:N], w, b, labels[:N], weights[:N], grad=grad)
+            outs = [torch.full_like(t, 7.0) for t in (want if grad else (want,))]
+            ptrs = [t.data_ptr() for t in outs] + [None] * (4 - len(outs))
+            assert lib.wind_label_loss(C.byref(lay), h.data_ptr(), H, labels.data_ptr(), weights.data_ptr(), N, *ptrs, ws.data_ptr(), size,
+                                       torch.cuda.current_stream().cuda_stream) == 0
+            torch.cuda.synchronize()
+            assert all(torch.equal(x, y) for x, y in zip(outs, want if grad else (want,))), (N, grad)
+    size = query("wind_transducer_loss_workspace_bytes", w, 6, 60, 20, 1)
+    ws = torch.full((size,), 0xFF, dtype=torch.uint8, device="cuda")
+    for B, T, U in ((6, 60, 20), (5, 60, 19), (6, 10, 20), (1, 1, 0), (6, 59, 20)):
+        e, p, _, _, y, frames, counts, weights = lattice(B, T, U, H, V1, dtype, 40 + T)
+        want = api().transducer_loss(e, p, w, b, y, frames, counts, weights, grad=GRAD)
+        outs = [torch.full_like(t, 7.0) for t in want]
+        assert lib.wind_transducer_loss(C.byref(lay), e.data_ptr(), e.stride(0), e.stride(1), p.data_ptr(), p.stride(0), p.stride(1), y.data_ptr(), frames.data_ptr(),
+                                        counts.data_ptr(), weights.data_ptr(), B, T, U, *(t.data_ptr() for t in outs), ws.data_ptr(), size,
+                                        torch.cuda.current_stream().cuda_stream) == 0
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(outs, want)), (B, T, U)

@@ -45,3 +45,26 @@ def test_widths_out_of_range_are_refused(lib):  # noqa: F811
         for bad in (dict(V1=most + 1, H=32), dict(V1=32, H=most + 1)):
             assert rows_size(lib, layer(**bad), 8, grads=grads)[0] == WIND_ERR_UNSUPPORTED and b"2^23" in lib.wind_last_error()
             assert lattice_size(lib, layer(**bad), 1, 4, 2, grads=grads)[0] == WIND_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("V1,H,dtype,K", [(65537, 48, 1, 1), (65537, 2048, 1, 1), (4097, 640, 1, 16), (1025, 640, 0, 64), (33, 64, 0, 1), (8193, 1024, 1, 16), (50, 40, 1, 3)])
+def test_a_workspace_for_many_rows_serves_fewer(lib, V1, H, dtype, K):  # noqa: F811
+    """Also across the sizes where tiles, parts of sums, chunks and the sorting of entries change; and one for steps serves scores."""
+    lay, last = layer(V1=V1, H=H, dtype=dtype), 0
+    sizes = sorted({max(0, int(2 ** (x / 16)) + d) for x in range(0, 350) for d in (-1, 0, 1)} | set(range(9000, 12000, 64)))
+    for N in sizes:
+        need = rows_size(lib, lay, N, K=K)[1]
+        assert need >= last, N
+        assert rows_size(lib, lay, N, K=K, grads=0)[1] <= need
+        last = need
+
+
+@pytest.mark.parametrize("V1,H,dtype", [(1025, 640, 1), (33, 64, 0), (4097, 640, 1), (5000, 200, 0)])
+def test_a_workspace_for_large_lattices_serves_smaller(lib, V1, H, dtype):  # noqa: F811
+    lay = layer(V1=V1, H=H, dtype=dtype)
+    steps = [0, 1, 2, 3, 7, 16, 17, 40, 63, 64, 65, 127, 128, 250, 256, 257, 700, 1023, 1024, 1100]
+    for grads in (0, 1):
+        for size in (lambda x: (x + 1, 250, 40), lambda x: (16, x, 40), lambda x: (3, 300, x), lambda x: (2, x, 1100), lambda x: (16, 2 * x, x // 4)):
+            needs = [lattice_size(lib, lay, *size(x), grads=grads)[1] for x in steps]
+            assert needs == sorted(needs), needs
+    assert all(lattice_size(lib, lay, b, 250, 40, grads=0)[1] <= lattice_size(lib, lay, b, 250, 40)[1] for b in range(1, 40))
