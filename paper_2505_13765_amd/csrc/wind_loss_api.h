@@ -258,7 +258,7 @@ int loss_layer_check(const wind_output_layer *l) {
   if (l->dtype != WIND_F32 && l->dtype != WIND_BF16) return fail(WIND_ERR_ARG, "dtype must be WIND_F32 or WIND_BF16");
   if (l->w_stride < l->H) return fail(WIND_ERR_ARG, "w_stride must be at least H");
   if ((uintptr_t)l->w % (l->dtype ? 2 : 4) || (uintptr_t)l->b % 4) return fail(WIND_ERR_ARG, "w or b is not aligned to its type");
-  if ((long long)((l->V1 + 31) / 32 * 32) * ((l->H + 31) / 32 * 32) >= 1ll << 31) return fail(WIND_ERR_UNSUPPORTED, "V1 * H must be below 2^31");
+  if ((l->V1 + 31ll) / 32 * 32 * ((l->H + 31ll) / 32 * 32) >= 1ll << 31) return fail(WIND_ERR_UNSUPPORTED, "V1 * H must be below 2^31");
   return WIND_OK;
 }
 int loss_workspace_check(const LossPlan &p, const void *ws, size_t bytes) {

@@ -68,3 +68,13 @@ def test_a_workspace_for_large_lattices_serves_smaller(lib, V1, H, dtype):  # no
             needs = [lattice_size(lib, lay, *size(x), grads=grads)[1] for x in steps]
             assert needs == sorted(needs), needs
     assert all(lattice_size(lib, lay, b, 250, 40, grads=0)[1] <= lattice_size(lib, lay, b, 250, 40)[1] for b in range(1, 40))
+
+
+def test_widths_near_the_integers_end_are_refused(lib):  # noqa: F811
+    """Rounding them up to whole panels must not leave the integers' range."""
+    from paper_2505_13765_amd.binding import WIND_ERR_UNSUPPORTED
+
+    for top in ((1 << 31) - 1, (1 << 31) - 31, (1 << 31) - 32):
+        for bad in (dict(V1=top, H=1, stride=1), dict(V1=2, H=top)):
+            assert rows_size(lib, layer(**bad), 8)[0] == WIND_ERR_UNSUPPORTED, bad
+            assert lattice_size(lib, layer(**bad), 1, 4, 2)[0] == WIND_ERR_UNSUPPORTED, bad
