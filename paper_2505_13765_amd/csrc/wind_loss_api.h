@@ -568,8 +568,8 @@ int wind_distill_loss(const wind_output_layer *layer, const void *h, int64_t h_s
   if (rc) return rc;
   if (N && !teacher_logits) return fail(WIND_ERR_ARG, "null argument");
   if (K < 1) return fail(WIND_ERR_ARG, "K >= 1 required");
-  if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.f / temperature))
-    return fail(WIND_ERR_ARG, "temperature must be positive and finite");
+  if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(kLog2e * (1.f / temperature)))
+    return fail(WIND_ERR_ARG, "temperature must be positive and finite, and so must log2(e) / temperature");
   LossRowsDev rows{};
   rows.kind = kLossDistill;
   rows.K = K;

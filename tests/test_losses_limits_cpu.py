@@ -78,3 +78,12 @@ def test_widths_near_the_integers_end_are_refused(lib):  # noqa: F811
         for bad in (dict(V1=top, H=1, stride=1), dict(V1=2, H=top)):
             assert rows_size(lib, layer(**bad), 8)[0] == WIND_ERR_UNSUPPORTED, bad
             assert lattice_size(lib, layer(**bad), 1, 4, 2)[0] == WIND_ERR_UNSUPPORTED, bad
+
+
+@pytest.mark.parametrize("tau", (4e-39, 4.2e-39, 3e-39))
+def test_temperatures_whose_scale_overflows_are_refused(lib, tau):  # noqa: F811
+    """log2(e) / tau is what logits are multiplied with.  The buffers are made up: the call must not get further than its arguments."""
+    from paper_2505_13765_amd.binding import WIND_ERR_ARG
+
+    assert lib.wind_distill_loss(C.byref(layer()), 4096, 64, 4096, 4096, 2, tau, None, 8, 4096, None, None, None, 4096 + 1, 1 << 40, None) == WIND_ERR_ARG
+    assert b"temperature" in lib.wind_last_error()
