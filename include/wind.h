@@ -400,7 +400,7 @@ int wind_label_loss(const wind_output_layer *layer, const void *h, int64_t h_str
  * Distillation from a teacher's K largest logits: with q the softmax of a row's teacher logits / temperature over its entries and
  * p the softmax of x / temperature over all outputs, loss[n] = temperature^2 sum_k q_k (log q_k - log p_label_k).
  *   teacher_labels, teacher_logits   DEVICE [N, K] int32 / fp32.  Entries with a negative label or a logit of -inf are not there; a row
- *               without any is left out (loss 0, no gradient); one with a label >= V1 is left out and its loss is NaN.  An output may be named
+ *               without any is left out (loss 0, no gradient); one with a label >= V1, whatever its logit, is left out and its loss is NaN.  An output may be named
  *               twice: both entries count.  (wind_beam_window_scores returns such lists; K <= 1024)
  */
 int wind_distill_loss(const wind_output_layer *layer, const void *h, int64_t h_stride, const int32_t *teacher_labels, const float *teacher_logits, int K,
@@ -421,7 +421,8 @@ int wind_transducer_loss_workspace_bytes(const wind_output_layer *layer, int B, 
  *               has loss +inf and no gradient.  (Probabilities are kept down to 2^-268000000 or so, losses of 186 million; a path below that, as
  *               through an output that b masks with -1e9, counts as impossible)
  *   loss        DEVICE [B] fp32;  de [B, T, H], dp [B, U + 1, H] (zeros beyond frames and label_counts), dw [V1, H], db [V1]
- * U <= 4095, T * (U + 1) < 2^27, B * T * (U + 1) < 2^31 and B * (T + U + 1) * H / 64 < 2^31 (WIND_ERR_UNSUPPORTED).
+ * B >= 1.  U <= 4095, T * (U + 1) < 2^27, B * T * (U + 1) and B * (U + 64) < 2^31, with gradients B * (T + U + 1) * ceil(H / 256) + ceil(V1 / 16) + 2048
+ * below 2^24 (WIND_ERR_UNSUPPORTED).
  */
 int wind_transducer_loss(const wind_output_layer *layer, const void *e, int64_t e_stride_b, int64_t e_stride_t, const void *p, int64_t p_stride_b,
                          int64_t p_stride_u, const int32_t *labels, const int32_t *frames, const int32_t *label_counts, const float *weights, int B, int T,

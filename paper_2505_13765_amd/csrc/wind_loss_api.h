@@ -38,6 +38,7 @@ struct LossTiles<3, 3> {
 // rows of 65537 outputs (512 MB) left the products of few tiles: 8.9 ms for 7373 rows, one chunk 7.4
 constexpr size_t kLossChunkBytes = 1200u << 20, kLossStatBytes = 512u << 20;
 constexpr int kLossMaxEntries = 1024;
+constexpr int kLossJoinBlocks = 2048;   // workgroups, at most, that add up dW's parts
 // Entries (of all rows) and column blocks up to which a row tile's last workgroup joins its column blocks: one launch less, 36 -> 31 us for 16 rows of 1025
 // outputs.  With more, that workgroup is what the others' results wait for (3001 rows of 64 entries: 73 us against 51 and 6).
 constexpr long long kLossJoinEntries = 4096;
@@ -408,7 +409,7 @@ LossFinish loss_gradients(const LossRun &r, int chunk, bool dz, LossOut dz_out, 
     if (p.dw_direct) wo = LossOut{dw, (size_t)p.H, p.dtype, p.H, nullptr, 0, 1, 0};
     else if (chunk + 1 == p.chunks) {
       f.dw = LossJoin{r.at<float>(p.dw), p.w.splits, wo.part, wo.ld, p.V1, p.H, p.dtype, nullptr, dw};
-      f.n_dw = (int)loss_blocks((size_t)p.V1 * (p.hd / 4), 256, 2048);
+      f.n_dw = (int)loss_blocks((size_t)p.V1 * (p.hd / 4), 256, kLossJoinBlocks);
     }
   }
   const LossProduct z{dx, r.w, p.vblk, p.H, (p.H + p.z.bn - 1) / p.z.bn}, w{dx, r.x, 0, p.V1, (p.H + p.w.bn - 1) / p.w.bn};
@@ -501,7 +502,10 @@ int lattice_plan(LossPlan &p, const wind_output_layer *layer, int B, int T, int 
   if (B < 1 || T < 0 || U < 0) return fail(WIND_ERR_ARG, "B >= 1, T >= 0 and U >= 0 required");
   if (U > 4095) return fail(WIND_ERR_UNSUPPORTED, "U must be at most 4095");
   if ((double)T * (U + 1.0) >= 134217728.0) return fail(WIND_ERR_UNSUPPORTED, "T * (U + 1) must be below 2^27");
-  if ((double)B * T * (U + 1.0) >= 2147483648.0 || (double)B * ((double)T + U + 1.0) * ((layer->H + 63) / 64) >= 2147483648.0) return fail(WIND_ERR_UNSUPPORTED, "B * T * (U + 1) and B * (T + U + 1) * H / 64 must be below 2^31");
+  if ((double)B * T * (U + 1.0) >= 2147483648.0 || (double)B * (U + 64.0) >= 2147483648.0) return fail(WIND_ERR_UNSUPPORTED, "B * T * (U + 1) and B * (U + 64) must be below 2^31");
+  // (the largest launch, lattice_finish_kernel's, has fewer than 2^24 workgroups of 256 threads: a column block of a frame or prediction row each, db's and dW's)
+  if (grads && (double)B * ((double)T + U + 1.0) * ((layer->H + 255ll) / 256) + (layer->V1 + 15ll) / 16 + kLossJoinBlocks >= 16777216.0)
+    return fail(WIND_ERR_UNSUPPORTED, "gradients need B * (T + U + 1) * ceil(H / 256) + ceil(V1 / 16) + 2048 below 2^24");
   p.kind = kLossLattice;
   p.dtype = layer->dtype;
   p.V1 = layer->V1;

@@ -87,3 +87,17 @@ def test_temperatures_whose_scale_overflows_are_refused(lib, tau):  # noqa: F811
 
     assert lib.wind_distill_loss(C.byref(layer()), 4096, 64, 4096, 4096, 2, tau, None, 8, 4096, None, None, None, 4096 + 1, 1 << 40, None) == WIND_ERR_ARG
     assert b"temperature" in lib.wind_last_error()
+
+
+def test_lattices_whose_launches_would_not_fit_are_refused(lib):  # noqa: F811
+    """A launch has fewer than 2^32 threads: the sums of a gradient's frames and prediction rows take 256 for each 256 columns of one.  Scores have none."""
+    from paper_2505_13765_amd.binding import WIND_ERR_UNSUPPORTED, WIND_OK
+
+    for lay, most in ((layer(V1=33, H=640), ((1 << 24) - 2048 - 3) // 3), (layer(V1=33, H=64), (1 << 24) - 2048 - 4)):
+        for B in (1, 8):
+            T = most // B - 2
+            assert lattice_size(lib, lay, B, T, 1)[0] == WIND_OK
+            assert lattice_size(lib, lay, B, T + 2, 1)[0] == WIND_ERR_UNSUPPORTED and b"2^24" in lib.wind_last_error()
+            assert lattice_size(lib, lay, B, T + 2, 1, grads=0)[0] == WIND_OK
+    assert lattice_size(lib, layer(), 1 << 25, 1, 0, grads=0)[0] == WIND_ERR_UNSUPPORTED     # 64 threads for each recursion
+    assert lattice_size(lib, layer(), (1 << 25) - 1, 1, 0, grads=0)[0] == WIND_OK
