@@ -7,6 +7,9 @@ stream, and nothing waits, allocates outside torch or comes back to the host, so
 
 Each function returns the losses, or, with `grad` (names of the inputs whose gradients are wanted), a tuple of the losses and
 those gradients in the order asked for: the gradients of sum(weights * losses), `weights` None counting as ones.
+
+There is no autograd graph behind either: hand the gradients on (`torch.autograd.backward((e, p), (de, dp))`, or to the optimiser).  A call without `grad` on tensors
+that require gradients is refused where autograd records, since its losses would silently be constants; score under `torch.no_grad()`.
 """
 from __future__ import annotations
 
@@ -59,17 +62,21 @@ def _on(device):
     return torch.cuda.device(device) if device.index != torch.cuda.current_device() else contextlib.nullcontext()
 
 
-def _asked(grad, names):
+def _asked(grad, names, inputs):
+    import torch
+
     grad = tuple(grad or ())
     if any(g not in names for g in grad) or len(set(grad)) != len(grad):
         raise ValueError(f"grad takes each of {names} at most once")
+    if not grad and torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in inputs):
+        raise ValueError("the losses have no autograd graph: ask for gradients with grad=..., or call under torch.no_grad()")
     return grad
 
 
 def _row_loss(kind, h, w_out, b_out, labels, logits, temperature, weights, grad):
     import torch
 
-    layer, grad = _layer(w_out, b_out), _asked(grad, ("h", "w", "b"))
+    grad, layer = _asked(grad, ("h", "w", "b"), (h, w_out, b_out, logits, weights)), _layer(w_out, b_out)
     (V1, H), device = w_out.shape, w_out.device
     if h.dim() != 2 or labels.dim() != (1 if kind == "label" else 2):
         raise ValueError("h must be [N, H], labels [N], teacher labels [N, K]")
@@ -118,7 +125,7 @@ def transducer_loss(e, p, w_out, b_out, labels, frames, label_counts, weights=No
     [B, U], frames [B] and label_counts [B] (all int32).  grad: of "e", "p", "w", "b"."""
     import torch
 
-    layer, grad = _layer(w_out, b_out), _asked(grad, ("e", "p", "w", "b"))
+    grad, layer = _asked(grad, ("e", "p", "w", "b"), (e, p, w_out, b_out, weights)), _layer(w_out, b_out)
     (V1, H), device = w_out.shape, w_out.device
     if e.dim() != 3 or p.dim() != 3 or labels.dim() != 2 or p.shape[1] < 1:
         raise ValueError("e must be [B, T, H], p [B, U + 1, H] and labels [B, U]")

@@ -101,3 +101,27 @@ def test_lattices_whose_launches_would_not_fit_are_refused(lib):  # noqa: F811
             assert lattice_size(lib, lay, B, T + 2, 1, grads=0)[0] == WIND_OK
     assert lattice_size(lib, layer(), 1 << 25, 1, 0, grads=0)[0] == WIND_ERR_UNSUPPORTED     # 64 threads for each recursion
     assert lattice_size(lib, layer(), (1 << 25) - 1, 1, 0, grads=0)[0] == WIND_OK
+
+
+def test_losses_without_a_graph_are_not_taken_for_ones_with():
+    """Where autograd would expect a graph (no gradients asked for, an input that requires them), the call says that there is none; with gradients asked for, or outside
+    autograd's recording, it goes on (here: to the next refusal, no GPU)."""
+    import torch
+
+    from paper_2505_13765_amd import distill_loss, label_loss, transducer_loss
+
+    h, w, lab = torch.zeros(3, 4), torch.zeros(5, 4), torch.zeros(3, dtype=torch.int32)
+    leaf = lambda t: t.clone().requires_grad_()  # noqa: E731
+    calls = (lambda f, **k: label_loss(f(h), w, None, lab, **k), lambda f, **k: label_loss(h, f(w), None, lab, **k),
+             lambda f, **k: label_loss(h, w, f(torch.zeros(5)), lab, **k), lambda f, **k: label_loss(h, w, None, lab, weights=f(torch.ones(3)), **k),
+             lambda f, **k: distill_loss(h, w, None, lab[:, None], f(torch.zeros(3, 1)), **k),
+             lambda f, **k: transducer_loss(f(h[None]), h[None], w, None, lab[None, :2], lab[:1], lab[:1], **k),
+             lambda f, **k: transducer_loss(h[None], f(h[None]), w, None, lab[None, :2], lab[:1], lab[:1], **k))
+    for call in calls:
+        with pytest.raises(ValueError, match="no autograd graph"):
+            call(leaf)
+        for go_on in (lambda: call(leaf, grad=("w",)), lambda: call(lambda t: t)):
+            with pytest.raises(ValueError, match="GPU"):
+                go_on()
+        with torch.no_grad(), pytest.raises(ValueError, match="GPU"):
+            call(leaf)
