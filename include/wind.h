@@ -360,8 +360,8 @@ int wind_get_route_counts(wind_model *m, wind_route_counts *out);
  * the last of the V1 outputs.  No call keeps logits or their gradient for all rows: both are formed in pieces inside the workspace.
  *   dtype       WIND_BF16 or WIND_F32: type of w, of the rows (h, or e and p) and of their gradients; products are summed in fp32,
  *               fp32 operands are multiplied to 2^-23 relative.  b, db, weights and losses are fp32.  WIND_BF16 rounds, beside the results
- *               dh, de, dp and dw themselves: the logits' gradient to bf16 before it is multiplied with w and the rows (2^-8 of each value at most; to
- *               16 bits where up to 128 rows count in all), and the transducer's hidden rows relu(e + p) to 16 bits before they are multiplied with w
+ *               dh, de, dp and dw themselves: the logits' gradient to bf16 before it is multiplied with w and the rows (2^-8 of each value at most, but
+ *               for a weight that all rows share; to 16 bits where up to 128 rows count in all), and the transducer's hidden rows relu(e + p) to 16 bits before they are multiplied with w
  *               and to bf16 before they go into dw.  Losses and db see only the 16 bits.  WIND_F32 has none of these roundings
  * Common arguments:
  *   weights     DEVICE fp32, may be NULL (ones): the gradients are those of the sum over rows (utterances) of weight x loss; the

@@ -392,7 +392,7 @@ LossFinish loss_gradients(const LossRun &r, int chunk, bool dz, LossOut dz_out, 
   });
   LossFinish f{};
   if (db) {
-    f.db = LossDb{d.colsum, p.vblk * 32, p.V1, p.x.bm, chunk > 0, db};
+    f.db = LossDb{d.colsum, p.vblk * 32, p.V1, p.x.bm, chunk > 0, p.pd == 1, db};
     f.n_db = (p.V1 + 15) / 16;
   }
   const PanelsDev dx{d.dx, d.plane, (uint32_t)p.R, (uint32_t)p.vblk};

@@ -708,6 +708,17 @@ struct LossDx {
 // The row tiles of few rows end at 256 at the latest, and the space of one plane of all rows (512 at least) holds both of theirs.
 constexpr int kLossFinePanel = 256;
 __device__ __forceinline__ bool loss_fine(int may_fine, const LossChunk &k) { return may_fine && *k.count <= kLossFineRows; }
+// What dx on one plane is kept in units of: the mantissa (1 <= unit < 2) of the first scale that is not zero, of the chunk's first 64.  A weight that all rows share (1 / N)
+// is then not part of what is rounded: most rows' label has p - 1, near -1, and times such a weight all of them were rounded the same way, up to 2^-8 of the whole
+// gradient (971 rows of weight 1 / 971: error of dz 0.0027 of its norm, in units 0.0020; 466 rows 0.0035, 0.0019; the result's own rounding 0.0017).  The products' results are multiplied by it.
+__device__ __forceinline__ float loss_unit(const LossChunk &k, int live) {
+  const int lane = threadIdx.x & 63;
+  const float s = lane < live ? fabsf(k.scale[lane]) : 0.f;
+  const unsigned long long some = __ballot(s >= 1.17549435e-38f && s < __builtin_inff());
+  if (!some) return 1.f;
+  const unsigned bits = (unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(s), __builtin_ctzll(some));
+  return __uint_as_float(0x3F800000u | (bits & 0x007FFFFFu));
+}
 
 template <class T>
 __device__ __forceinline__ void loss_dx(const LossProduct &g, const LossChunk &k, const float *bias, const LossDx &d, int row0, int j0, int part0, unsigned char *smem) {
@@ -721,13 +732,15 @@ __device__ __forceinline__ void loss_dx(const LossProduct &g, const LossChunk &k
     loss_bias<T>(bias, g.cols, col0, acc);
   });
   float *tile = reinterpret_cast<float *>(smem) + wave * 32 * T::PITCH;
-  const bool fine = loss_fine(d.may_fine, k);
+  constexpr bool F32 = T::PA == 3;   // (three planes always)
+  const bool fine = !F32 && loss_fine(d.may_fine, k);
+  const float per_unit = !F32 && d.may_fine && !fine ? 1.f / loss_unit(k, chunk_rows(k)) : 1.f;
   const int planes = fine ? 2 : d.planes;
   const size_t panel = (size_t)(fine ? kLossFinePanel : k.R) * 32, plane = fine ? panel * d.blocks : d.plane;
 #pragma unroll
   for (int mi = 0; mi < T::MI; ++mi) {
     const int i = i0 + 32 * mi;
-    const float s = k.scale[i], top = k.top[i], norm = k.norm[i];
+    const float s = k.scale[i] * per_unit, top = k.top[i], norm = k.norm[i];
 #pragma unroll
     for (int ni = 0; ni < T::NI; ++ni)
 #pragma unroll
@@ -744,15 +757,15 @@ __device__ __forceinline__ void loss_dx(const LossProduct &g, const LossChunk &k
           if (x > 0 && list[x - 1] >> 12 == w >> 12) continue;
           const int row_x = (int)(w >> 12) & 31;
           float &at = tile[row_x * T::PITCH + (int)(w >> 18)];
-          float v = at - coef[(size_t)(w & 4095u) * k.R + row_x];
-          for (int y = x + 1; y < n && list[y] >> 12 == w >> 12; ++y) v -= coef[(size_t)(list[y] & 4095u) * k.R + row_x];
+          float v = at - coef[(size_t)(w & 4095u) * k.R + row_x] * per_unit;
+          for (int y = x + 1; y < n && list[y] >> 12 == w >> 12; ++y) v -= coef[(size_t)(list[y] & 4095u) * k.R + row_x] * per_unit;
           at = v;
         }
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
       } else if (k.K <= 2) {
         const int at[2] = {entries.label[mi][0] - col0, entries.label[mi][1] - col0};
-        const float c[2] = {k.coef[i], k.K > 1 ? k.coef[k.R + i] : 0.f};
+        const float c[2] = {k.coef[i] * per_unit, k.K > 1 ? k.coef[k.R + i] * per_unit : 0.f};
         if (half == 0) {
 #pragma unroll
           for (int e = 0; e < 2; ++e)
@@ -763,7 +776,7 @@ __device__ __forceinline__ void loss_dx(const LossProduct &g, const LossChunk &k
         float c[8];
         entries.batch(k, i, e0, col0, at);
 #pragma unroll
-        for (int x = 0; x < 8; ++x) c[x] = e0 + 8 * half + x < k.K ? k.coef[(size_t)(e0 + 8 * half + x) * k.R + i] : 0.f;
+        for (int x = 0; x < 8; ++x) c[x] = e0 + 8 * half + x < k.K ? k.coef[(size_t)(e0 + 8 * half + x) * k.R + i] * per_unit : 0.f;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {   // one lane of a row after the other: an output that is named twice is taken off twice, in order
           if (half == h) {
@@ -858,7 +871,7 @@ struct LossOut {
 };
 // 32 rows of results from LDS, RUN values of a row per lane
 template <int RUN>
-__device__ __forceinline__ void loss_store_rows(const LossOut &o, const float *tile, int pitch, int width, int i0, int rows, int j0, size_t base) {
+__device__ __forceinline__ void loss_store_rows(const LossOut &o, const float *tile, int pitch, int width, int i0, int rows, int j0, size_t base, float unit) {
   const int lane = threadIdx.x & 63, per = width / RUN;
   for (int u = lane; u < 32 * per; u += 64) {
     const int r = u / per, c = (u - r * per) * RUN, i = i0 + r, j = j0 + c;
@@ -866,7 +879,7 @@ __device__ __forceinline__ void loss_store_rows(const LossOut &o, const float *t
     const size_t at = base + (size_t)(o.idx ? o.idx[i] : i) * o.ld + j;
     float v[RUN];
 #pragma unroll
-    for (int e = 0; e < RUN; ++e) v[e] = tile[r * pitch + c + e];
+    for (int e = 0; e < RUN; ++e) v[e] = tile[r * pitch + c + e] * unit;
     const bool whole = j + RUN <= o.cols;
     if constexpr (RUN == 8) {
       bf16_t *d = (bf16_t *)o.p + at;
@@ -890,7 +903,7 @@ __device__ __forceinline__ void loss_store_rows(const LossOut &o, const float *t
 // A wave's results, 32 rows at a time through LDS: what a store instruction writes is then whole lines of a few rows, not a piece of 32 of them
 // (dW of 43250 x 654 for 9 rows: 89 us by pieces).
 template <class T>
-__device__ __forceinline__ void loss_store(const LossOut &o, const f32x16 (&acc)[T::MI][T::NI], int i0, int rows, int j0, int split, unsigned char *smem) {
+__device__ __forceinline__ void loss_store(const LossOut &o, const f32x16 (&acc)[T::MI][T::NI], int i0, int rows, int j0, int split, float unit, unsigned char *smem) {
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   float *tile = reinterpret_cast<float *>(smem) + wave * 32 * T::PITCH;
   const int j = j0 + (wave & 1) * 32 * T::NI;
@@ -901,8 +914,8 @@ __device__ __forceinline__ void loss_store(const LossOut &o, const f32x16 (&acc)
     if (i >= rows) break;
     loss_tile_out<T>(acc[mi], tile);
     const size_t base = (size_t)split * o.part;
-    if (o.dtype) loss_store_rows<8>(o, tile, T::PITCH, 32 * T::NI, i, rows, j, base);
-    else loss_store_rows<4>(o, tile, T::PITCH, 32 * T::NI, i, rows, j, base);
+    if (o.dtype) loss_store_rows<8>(o, tile, T::PITCH, 32 * T::NI, i, rows, j, base, unit);
+    else loss_store_rows<4>(o, tile, T::PITCH, 32 * T::NI, i, rows, j, base, unit);
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
   }
@@ -918,21 +931,21 @@ __device__ __forceinline__ void loss_clear(f32x16 (&acc)[T::MI][T::NI]) {
 
 // A product whose K axis several workgroups may share: tiles of o.splits parts.
 template <class T, bool TA, bool TB>
-__device__ __forceinline__ void loss_product(int bid, const LossProduct &g, const LossOut &o, int rows, int slabs, unsigned char *smem) {
+__device__ __forceinline__ void loss_product(int bid, const LossProduct &g, const LossOut &o, int rows, int slabs, float unit, unsigned char *smem) {
   int ti, tj, split;
   if (!loss_place(bid, (rows + T::BM - 1) / T::BM, g.ct, o.splits, ti, tj, split)) return;
   const int per = (slabs + o.splits - 1) / o.splits, s0 = min(split * per, slabs), s1 = min(s0 + per, slabs);
   f32x16 acc[T::MI][T::NI];
   if (s0 < s1) loss_mainloop<T, TA, TB>(g.a, g.b, ti * T::BM, tj * T::BN, s0, s1, smem, acc, [&]() { loss_clear<T>(acc); });
   else loss_clear<T>(acc);
-  loss_store<T>(o, acc, ti * T::BM, rows, tj * T::BN, split, smem);
+  loss_store<T>(o, acc, ti * T::BM, rows, tj * T::BN, split, unit, smem);
 }
 // dz = dx W: rows of the chunk against columns of W's panels, summed over outputs.  dW = dx^T z: columns of dx's panels against columns of z's, summed over
 // the chunk's rows.  In one launch, on tiles of one shape.
 template <class T>
-__device__ __forceinline__ void loss_products(const LossProduct &z, const LossOut &zo, int z_blocks, const LossProduct &w, const LossOut &wo, int live, unsigned char *smem) {
-  if ((int)blockIdx.x < z_blocks) loss_product<T, false, true>((int)blockIdx.x, z, zo, live, z.slabs, smem);
-  else if (!wo.add || live) loss_product<T, true, true>((int)blockIdx.x - z_blocks, w, wo, w.cols, (live + 31) / 32, smem);
+__device__ __forceinline__ void loss_products(const LossProduct &z, const LossOut &zo, int z_blocks, const LossProduct &w, const LossOut &wo, int live, float unit, unsigned char *smem) {
+  if ((int)blockIdx.x < z_blocks) loss_product<T, false, true>((int)blockIdx.x, z, zo, live, z.slabs, unit, smem);
+  else if (!wo.add || live) loss_product<T, true, true>((int)blockIdx.x - z_blocks, w, wo, w.cols, (live + 31) / 32, unit, smem);
 }
 // F: the tile of the same shape for dx on two planes, where that is decided by the rows that count; else T.
 template <class T, class F>
@@ -944,22 +957,24 @@ __global__ __launch_bounds__(256, T::W) void loss_products_kernel(LossProduct z,
     if (loss_fine(1, k)) {
       z.a.rows = w.a.rows = kLossFinePanel;
       z.a.plane = w.a.plane = (size_t)kLossFinePanel * 32 * z.a.blocks;
-      loss_products<F>(z, zo, z_blocks, w, wo, live, smem);
+      loss_products<F>(z, zo, z_blocks, w, wo, live, 1.f, smem);
       return;
     }
-  }
-  loss_products<T>(z, zo, z_blocks, w, wo, live, smem);
+    loss_products<T>(z, zo, z_blocks, w, wo, live, loss_unit(k, live), smem);
+  } else loss_products<T>(z, zo, z_blocks, w, wo, live, 1.f, smem);
 }
 
 // ---- the last launch of a chunk -----------------------------------------------------------------
 // db: the column sums of all row tiles.  A workgroup takes 16 columns, 16 threads each.
 struct LossDb {
   const float *colsum;
-  int width, cols, tile_rows, add;
+  int width, cols, tile_rows, add, may_fine;
   float *db;
 };
-__device__ __forceinline__ void loss_db(const LossDb &d, int live, int block) {
+__device__ __forceinline__ void loss_db(const LossDb &d, const LossChunk &k, int block) {
   __shared__ float sums[16][16];
+  const int live = chunk_rows(k);
+  const float unit = d.may_fine && !loss_fine(1, k) ? loss_unit(k, live) : 1.f;
   const int parts = 2 * ((live + d.tile_rows - 1) / d.tile_rows);
   const int lane = threadIdx.x & 15, grp = threadIdx.x >> 4, v = block * 16 + lane;
   float s = 0.f;
@@ -973,6 +988,7 @@ __device__ __forceinline__ void loss_db(const LossDb &d, int live, int block) {
   s = 0.f;
 #pragma unroll
   for (int q = 0; q < 16; ++q) s += sums[q][lane];
+  s *= unit;
   d.db[v] = d.add ? d.db[v] + s : s;
 }
 
@@ -1014,7 +1030,7 @@ struct LossFinish {
 };
 // false: the workgroup's number, less those taken, is left in `block`
 __device__ __forceinline__ bool loss_finish(const LossFinish &f, const LossChunk &k, int &block) {
-  if (block < f.n_db) { loss_db(f.db, chunk_rows(k), block); return true; }
+  if (block < f.n_db) { loss_db(f.db, k, block); return true; }
   block -= f.n_db;
   if (block < f.n_dw) { loss_join(f.dw, f.dw.rows, block, f.n_dw); return true; }
   block -= f.n_dw;

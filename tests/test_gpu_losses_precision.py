@@ -58,3 +58,29 @@ def test_gradients_against_differences_along_them():
         assert bound < 0.02 * slope, (k, bound, slope)
         assert abs((mine[0] - mine[1]) / (2 * s) - slope) <= bound, (k, mine, bound)
         assert abs(along(got[1 + GRAD.index(k)]) - slope) <= 1e-4 * slope, (k, slope)
+
+
+@pytest.mark.parametrize("N,first", [(1000, 0), (5000, 40)])
+def test_a_weight_that_all_rows_share_is_not_rounded(N, first):
+    """bf16 gradients of many rows of the weight c = 1 + 2^-8, which lies between two bf16 values, behind `first` rows of weight zero.  dx / c is p_v to bf16, off by 2^-8 of it
+    at most, and p - 1 at the label, off by p or half a step below one, 2^-9, whichever is less; c itself is multiplied in fp32.  Times c before its rounding, every
+    row's label would be off by almost 2^-8.  Beside that, logits, products and the result's rounding as in test_few_rows_that_count_among_many."""
+    H, V1, c = 64, 4000, 1 + 2.0**-8
+    g = torch.Generator().manual_seed(N)
+    h, w = (0.25 * torch.randn(s, H, generator=g) for s in (N, V1))
+    b, labels, weights = 0.1 * torch.randn(V1, generator=g), torch.randint(0, V1, (N,), generator=g, dtype=torch.int32), torch.full((N,), c)
+    weights[:first] = 0
+    h, w = h.bfloat16(), w.bfloat16()
+    _, dh, dw, db = api().label_loss(h.cuda(), w.cuda(), b.cuda(), labels.cuda(), weights=weights.cuda(), grad=("h", "w", "b"))
+    h, w, b = h.double(), w.double(), b.double()
+    p, one = torch.softmax(h @ w.T + b, dim=1), torch.nn.functional.one_hot(labels.long(), V1).double()
+    weights = weights.double()[:, None]
+    dx = weights * (p - one)
+    logit = 2 * (H + 2) * 2.0**-24 * (h.abs() @ w.abs().T + b.abs()).amax(1, keepdim=True) + 2.0**-20
+    exact = weights * p * logit + 2.0**-22 * dx.abs()
+    off = exact + weights * torch.where(one > 0, p.clamp(max=2.0**-9), 2.0**-8 * p)
+    for got, ref, bound in ((dh, dx @ w, off @ w.abs() + (V1 + 8) * 2.0**-24 * (dx.abs() @ w.abs())),
+                            (dw, dx.T @ h, off.T @ h.abs() + (N + 8) * 2.0**-24 * (dx.abs().T @ h.abs()))):
+        err = (got.double().cpu() - ref).abs()
+        assert (err <= 2.0**-8 * (ref.abs() + bound) + bound + 2.0**-133).all(), (err - 2.0**-8 * ref.abs()).max()
+    assert ((db.double().cpu() - dx.sum(0)).abs() <= exact.sum(0) + (N + 40) * 2.0**-24 * dx.abs().sum(0)).all()
