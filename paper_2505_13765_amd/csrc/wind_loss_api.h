@@ -92,7 +92,7 @@ constexpr ProductShape kProductShapes[] = {
     {256, 256, 1, 7.0e6, 1.0, 12, 3.2e9}, {256, 128, 2, 8.7e6, 0.73, 10, 1.53e9}, {128, 128, 2, 8.2e6, 0.81, 12, 1.17e9}, {64, 64, 1, 2.2e6, 1.0, 10, 1.6e9}};
 constexpr ProductShape kProductShapesF32[] = {{128, 128, 1, 7.6e6, 1.0, 37, 1.64e9}, {64, 64, 2, 6.5e6, 0.56, 18, 1.1e9}};
 constexpr int kProductParts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
-constexpr size_t kLossPartBytes = 80u << 20;   // parts of a sum, at most (of the same 70 problems and 600 others none was picked that takes more than 70 MB)
+constexpr size_t kLossPartBytes = 80u << 20;   // parts of a sum, at most (of 600 problems, 1 to 16384 rows or 90000 nodes, 33 to 65537 outputs, 48 to 2048 units, none was picked that takes more than 70 MB)
 
 // when `slots` workgroups at a time end that take nz tiles of time a each, then nw of time b
 double products_end(long long nz, double a, long long nw, double b, long long slots) {
